@@ -346,6 +346,141 @@ SALT_API salt_status salt_fuse_centroid_timed(salt_ctx* ctx, int32_t table, int3
 SALT_API salt_status salt_adapter_gram(salt_ctx* ctx, const void* blob1, int32_t r1, const void* blob2,
                                        int32_t r2, double* out, void* stream);
 
+/* ---- base weights in 8 bits ---------------------------------------------------------------
+ * The product the apply adds to: y = x W_base, in 8-bit floating point (e4m3: 1 sign, 4
+ * exponent and 3 fraction bits, largest value 448) with an fp32 scale for each block of 128.
+ * A table's W [in][out] is held in blocks of 128 inputs x 128 outputs (the last ones of a row
+ * or column smaller), x is quantised by the call per token and 128 inputs.  For a block v with
+ * largest magnitude amax, in fp32 and rounded to nearest even:
+ *
+ *     s = max(amax * (1/448), 2^-126),     code = e4m3(v * (1 / s)),
+ *     y[t][o] <- rne( sum_kb s_x[t][kb] s_w[kb][o / 128] sum_{k in kb} xq[t][k] wq[k][o] ),
+ *
+ * accumulated in fp32.  A value that is not finite in x makes NaN of its token's y, one in W
+ * of the outputs of its block.  A centroid is fused into W (salt_fuse_centroid) before W is pinned.
+ *
+ * salt_pin_base: quantise table `table`'s W (device, context dtype, row-major [in][ldw], 16-byte
+ * aligned, ldw a multiple of 8 and >= out_dim) into the context, which keeps the codes (1 byte
+ * a weight, out_dim padded to 256).  The first call also allocates the scratch that
+ * products quantise x into (max_tokens x the widest in_dim bytes).  Enqueued on `stream`; W
+ * may be freed once the stream has passed it.
+ * salt_pin_base_fp8: the same from codes wq [out][ldq] (device, e4m3, row-major, 16-byte aligned,
+ * ldq a multiple of 8 and >= in_dim) and any fp32 scales [ceil(out / 128)][ceil(in / 128)].
+ * salt_read_base: the weight as it is held, code * scale, into w [in][ldw] in the context dtype.
+ * Errors: SALT_ERR_OUT_OF_RANGE (table; more than 2^31 codes of a table or of the scratch),
+ * SALT_ERR_INVALID_ARG (pointers, row length), SALT_ERR_OUT_OF_MEMORY, SALT_ERR_BAD_STATE
+ * (salt_read_base of a table that was never pinned). */
+SALT_API salt_status salt_pin_base(salt_ctx* ctx, int32_t table, const void* w, int64_t ldw, void* stream);
+SALT_API salt_status salt_pin_base_fp8(salt_ctx* ctx, int32_t table, const void* wq, int64_t ldq,
+                                       const float* scales, void* stream);
+SALT_API salt_status salt_read_base(salt_ctx* ctx, int32_t table, void* w, int64_t ldw, void* stream);
+
+/* ys[i] [T][out_dim] <- x W_base of tables[i] for i < n; every table reads the one x [T][in_dim]
+ * (q, k and v; gate and up), so all have one in_dim.  x, ys: device, context dtype, dense,
+ * 16-byte aligned; x and the ys must not overlap.  ys are written once, not read.
+ * 0 <= T <= max_tokens.  Enqueued on `stream`; nothing is allocated, and results are
+ * reproducible bit for bit.  The products of a context share its scratch: the library orders them,
+ * also across streams.  Errors: SALT_ERR_OUT_OF_RANGE (table, T), SALT_ERR_BAD_STATE (a base
+ * weight never pinned), SALT_ERR_INVALID_ARG; nothing is enqueued then. */
+SALT_API salt_status salt_base_product(salt_ctx* ctx, int32_t n, const int32_t* tables, int32_t T, const void* x,
+                                       void* const* ys, void* stream);
+
+/* ---- paged KV cache in 8 bits ---------------------------------------------------------------
+ * A pool of pages for the keys and values of every layer, quantised as they are written.  A page
+ * holds page_tokens tokens of all kv heads; a page number names the same page in every layer.
+ * Per token and kv head, over the head_dim values of k, and of v:
+ *   SALT_KV_E4M3: s = the smallest power of two with amax / s <= 448 (1 if amax = 0; at least
+ *                 2^-100), code = e4m3(x / s);
+ *   SALT_KV_INT8: s = max(amax * (1/127), 2^-100), code = rint(x * (1 / s)) in [-127, 127].
+ * A vector with a value that is not finite is kept as a scale of NaN: it reads back as NaN, and
+ * (k or v alike) makes NaN of every attention row that sees the token, and of no other. */
+typedef enum { SALT_KV_E4M3 = 0, SALT_KV_INT8 = 1 } salt_kv_format;
+typedef struct {
+  int32_t n_layers;          /* in [1, 1024]                                              */
+  int32_t n_heads;           /* query heads: 1 to 16 times n_kv_heads; query head h reads
+                                kv head h / (n_heads / n_kv_heads)                          */
+  int32_t n_kv_heads;        /* in [1, 256]                                               */
+  int32_t head_dim;          /* 64, 128 or 256                                            */
+  int32_t page_tokens;       /* a power of two in [16, 256]                               */
+  int32_t n_pages;           /* in [1, 2^23]                                              */
+  int32_t format;            /* salt_kv_format                                            */
+  int32_t flags;             /* reserved, must be 0                                       */
+} salt_kv_config;
+
+typedef struct salt_kv salt_kv;
+typedef struct salt_seqs salt_seqs;
+
+/* Bytes of the pool (host-only; 0 for an invalid configuration). */
+SALT_API size_t salt_kv_bytes(const salt_kv_config* cfg);
+/* The pool is allocated and cleared by the call and owned by the context (freed by salt_kv_destroy
+ * or salt_destroy; salt_kv_destroy waits for the device).  k, v, q and out are in the context's
+ * dtype.  Errors: SALT_ERR_INVALID_ARG (configuration), SALT_ERR_OUT_OF_MEMORY. */
+SALT_API salt_status salt_kv_create(salt_ctx* ctx, const salt_kv_config* cfg, salt_kv** out);
+SALT_API void salt_kv_destroy(salt_ctx* ctx, salt_kv* kv);
+
+/* The sequences of one step, set once and used by every layer: like a plan, an object that owns
+ * its device buffers (page tables, work items, partial results) for up to max_seqs sequences and
+ * domains together, max_tokens new tokens and max_pages page references.  Freed by
+ * salt_seqs_destroy (which waits for the device), with its cache, or with the context.  Its work,
+ * and that of a cache, is ordered by the library across streams; streams that are to run
+ * concurrently need objects of their own, and a cache each. */
+SALT_API salt_status salt_seqs_create(salt_ctx* ctx, salt_kv* kv, int32_t max_seqs, int32_t max_tokens,
+                                      int32_t max_pages, salt_seqs** out);
+SALT_API void salt_seqs_destroy(salt_ctx* ctx, salt_seqs* seqs);
+
+/* One batch (host arrays, read before the call returns).  Sequence i has len[i] tokens of its own in the pages
+ * pages[page_off[i]] .. pages[page_off[i + 1] - 1], in order, this step's q_len[i] new ones the
+ * last of them.  It stands behind the prefix of domain[i] (-1, or domain NULL: none), a run of
+ * prefix_len[d] tokens in pages of its own that any number of sequences share: the prompt
+ * common to the users of a domain (the groups by centroid of Sec. 3.3).  The prefix' tokens are in
+ * the cache already: a prefix is written as a sequence of its own.
+ * The step's rows are the new tokens of sequence 0, then 1, and so on: T = sum of q_len.
+ * q_len[i] > len[i] is allowed: the tokens before the sequence's first have no own keys and
+ * no place in the cache. */
+typedef struct {
+  int32_t n_seqs;
+  const int32_t* q_len;        /* [n_seqs]                                                 */
+  const int32_t* len;          /* [n_seqs]                                                 */
+  const int32_t* page_off;     /* [n_seqs + 1], from 0                                      */
+  const int32_t* pages;        /* [page_off[n_seqs]]                                       */
+  const int32_t* domain;       /* [n_seqs] in [-1, n_domains), or NULL                     */
+  int32_t n_domains;
+  const int32_t* prefix_len;   /* [n_domains]                                              */
+  const int32_t* prefix_off;   /* [n_domains + 1], from 0                                   */
+  const int32_t* prefix_pages; /* [prefix_off[n_domains]]                                  */
+} salt_seq_batch;
+/* Validates the batch on the host (every length and page), cuts the attention's work and enqueues one
+ * copy on `stream`.  Refused on a stream under capture (SALT_ERR_BAD_STATE): a recorded call serves the
+ * batch that was set when it was recorded, and is recorded anew for another.  Errors:
+ * SALT_ERR_OUT_OF_RANGE (counts, lengths, pages, domains), SALT_ERR_INVALID_ARG; the batch set
+ * before stays then. */
+SALT_API salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* seqs, const salt_seq_batch* batch, void* stream);
+
+/* Write the step's keys and values of one layer into the cache: row t of k and v is the step's
+ * token t, [n_kv_heads][head_dim], rows ldk / ldv elements apart (0: dense; else a multiple of
+ * 8), 16-byte aligned.  SALT_ERR_INVALID_ARG too if two sequences of the batch write into one page. */
+SALT_API salt_status salt_kv_write(salt_ctx* ctx, salt_seqs* seqs, int32_t layer, const void* k, int64_t ldk,
+                                   const void* v, int64_t ldv, void* stream);
+
+/* Read the cache back into plain rows, code * scale rounded once to the context dtype:
+ *   SALT_KV_NEW: the step's T new tokens (zeros for those without a place in the cache);
+ *   SALT_KV_OWN: all own tokens of sequence 0, then 1, and so on (sum of len rows). */
+typedef enum { SALT_KV_NEW = 0, SALT_KV_OWN = 1 } salt_kv_what;
+SALT_API salt_status salt_kv_read(salt_ctx* ctx, salt_seqs* seqs, int32_t layer, int32_t what, void* k, int64_t ldk,
+                                  void* v, int64_t ldv, void* stream);
+
+/* Attention of the step's tokens over the cache, one layer: out[t][h] = sum_j p_j v_j with p =
+ * softmax_j(scale q[t][h] . k_j), j over the whole prefix of the token's domain and its sequence's own
+ * tokens up to its own place.  The step's keys and values are written first (salt_kv_write).  A prefix
+ * that several short sequences share is read once for all of them.  A token without keys gives zeros.
+ *   q [T][n_heads][head_dim], out the same: context dtype, rows ldq / ldo elements apart
+ *   (0: dense; else a multiple of 8), 16-byte aligned; out may not overlap q.
+ * The softmax's maximum and sum and the sum over v are fp32.  Reproducible bit for bit.
+ * Errors of these three calls: SALT_ERR_BAD_STATE (no batch set), SALT_ERR_OUT_OF_RANGE (layer),
+ * SALT_ERR_INVALID_ARG (pointers, row lengths, scale not finite or <= 0). */
+SALT_API salt_status salt_attend(salt_ctx* ctx, salt_seqs* seqs, int32_t layer, const void* q, int64_t ldq,
+                                 void* out, int64_t ldo, float scale, void* stream);
+
 /* ---- centroid routing (host only) ------------------------------------------------------
  * Sec. 3.2: a user's dataset is routed to a centroid of the library, or to the
  * standard-LoRA fallback, from the token-normalised displacement norms N_k its

@@ -16,11 +16,13 @@
 #include <new>
 #include <string>
 #include <thread>
+#include <utility>
 #include <vector>
 
 #include "../../include/salt.h"
 #include "salt_internal.h"
 #include "salt_launch.h"
+#include "salt_serve.h"
 
 namespace {
 
@@ -191,6 +193,9 @@ struct salt_ctx {
   EventRing readers, loaders;
   std::vector<salt_plan*> plans;
   salt_plan* map_plan = nullptr;         // the plan salt_apply_map builds and applies
+  // objects of the operators around the apply (salt_serve.cpp), freed with the context
+  std::vector<std::pair<void*, salt::OwnedFree>> owned;
+  void* base = nullptr;                  // the base weights among them
   bool poisoned = false;
   std::string err;
 };
@@ -796,6 +801,44 @@ salt_status fuse_impl(salt_ctx* ctx, int32_t table, int32_t c, float gamma, void
 
 }  // namespace
 
+// ---- what salt_serve.cpp takes from a context (salt_serve.h) -----------------------------
+namespace salt {
+salt_status ctx_live(salt_ctx* c) {
+  SALT_LIVE(c);
+  return SALT_OK;
+}
+CtxView ctx_view(const salt_ctx* c) {
+  return CtxView{c->device, c->n_cu, c->cfg.dtype == SALT_BF16, c->cfg.max_tokens, c->cfg.n_tables, c->tables.data()};
+}
+salt_status ctx_fail(salt_ctx* c, salt_status s, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return fail(c, s, "%s", buf);
+}
+salt_status ctx_hip_fail(salt_ctx* c, hipError_t e, const char* what) { return hip_fail(c, e, what); }
+bool ctx_own(salt_ctx* c, void* obj, OwnedFree f) {
+  try {
+    c->owned.emplace_back(obj, f);
+  } catch (const std::bad_alloc&) {
+    return false;
+  }
+  return true;
+}
+bool ctx_owns(const salt_ctx* c, const void* obj) {
+  return std::any_of(c->owned.begin(), c->owned.end(), [&](const auto& o) { return o.first == obj; });
+}
+bool ctx_disown(salt_ctx* c, void* obj) {
+  const auto it = std::find_if(c->owned.begin(), c->owned.end(), [&](const auto& o) { return o.first == obj; });
+  if (it == c->owned.end()) return false;
+  c->owned.erase(it);
+  return true;
+}
+void*& ctx_base(salt_ctx* c) { return c->base; }
+}  // namespace salt
+
 extern "C" {
 
 const char* salt_status_str(salt_status s) {
@@ -980,6 +1023,7 @@ void salt_destroy(salt_ctx* ctx) {
   (void)hipSetDevice(ctx->device);
   (void)hipDeviceSynchronize();
   for (salt_plan* p : ctx->plans) free_plan(p);
+  for (const auto& o : ctx->owned) o.second(o.first);
   destroy_ctx_memory(ctx);
   delete ctx;
 }

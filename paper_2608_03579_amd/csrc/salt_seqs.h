@@ -1,0 +1,207 @@
+// How a batch of sequences is cut into the attention's work items.  Host arithmetic
+// on the batch's lengths alone: no HIP types and no pointers into device memory.
+//
+// A row is one (token, query head).  The rows of one kv head that read the same keys
+// form a row set: the new tokens of one sequence times the query heads of a kv head, or,
+// for a domain prefix that two or more sequences share, those of all of them.  A row
+// set is cut into row tiles of whole tokens, and the keys of a tile into runs ("pieces")
+// of whole key units; a work item is one piece of one tile, run once per kv head.  A
+// row whose keys are all in one piece is finished there; others leave (max, sum,
+// weighted values) per piece, which a second kernel joins.
+#pragma once
+
+#include <stdint.h>
+
+#include <algorithm>
+#include <vector>
+
+namespace salt {
+
+constexpr int kKeyUnit = 64;       // keys of a unit; prefix and own keys start units of their own
+constexpr int kRowTiles[3] = {16, 64, 128};   // rows of a tile, by item kind
+constexpr int kMaxGroup = 16;      // query heads that share a kv head: a token's rows fit a tile
+
+struct AttItem {
+  int32_t kind;            // rows of the tile: kRowTiles[kind]
+  int32_t n_rows;          // rows in use (per kv head)
+  int32_t tok0;            // the tile's first entry of the token order
+  int32_t pos0;            // own position of that token (>= 0 or below), or kAllKeys where the tile reads a prefix alone
+  int32_t pre_ref, pre_len;// the prefix' first page reference and its keys (0: none)
+  int32_t own_ref;         // the own keys' first page reference
+  int32_t own_end;         // own keys the tile's last token sees
+  int32_t unit0, unit1;    // the piece: units of the prefix, then of the own keys
+  int32_t out_row;         // first row of the partial results (of kv head 0), or -1: the rows are finished here
+  int32_t pad_;
+};
+constexpr int kAllKeys = 1 << 30;
+// Pieces of one token, to be joined: `n` partial rows per query head, in two runs (its
+// own item's, and its domain's).  Partial row of piece p, kv head k and row r of the
+// tile: row + (p * n_kv_heads + k) * stride + r.
+struct AttJoin {
+  int32_t tok;
+  int32_t row[2], n[2], stride[2], r0[2];   // r0: the token's first row in the tile
+  int32_t pad_;
+};
+
+struct SeqBatch {
+  int n_seqs, n_domains;
+  const int32_t* q_len;
+  const int32_t* len;
+  const int32_t* page_off;     // sequences' page references, behind the domains'
+  const int32_t* domain;       // may be null
+  const int32_t* prefix_len;
+  const int32_t* prefix_off;
+};
+
+struct AttWork {
+  std::vector<AttItem> items;  // by kind, the longest first
+  int n_kind[3];
+  std::vector<int32_t> order;  // token order of the shared row sets, behind the identity [0, T)
+  std::vector<AttJoin> joins;
+  int64_t rows;                // partial rows
+};
+
+inline int seq_cdiv(int a, int b) { return (a + b - 1) / b; }
+
+// Rows that a sequence brings alone from which on it keeps its prefix to itself: a
+// tile of its own rows is full then, and sharing would only add a join.
+constexpr int kOwnRows = 128;
+
+struct AttTile {
+  AttItem it;
+  int units, n_tok;
+};
+
+// Partial rows that a plan of at most T tokens can need beyond two per row (pieces of
+// long key runs): the cut below keeps to it.
+constexpr int64_t kExtraRows = 1 << 16;
+
+// n_cu: compute units.  T: tokens of the batch (sum of q_len).
+inline void cut_attention(const SeqBatch& b, int T, int heads, int kv_heads, int n_cu, AttWork& w) {
+  const int gs = heads / kv_heads;
+  w.items.clear();
+  w.joins.clear();
+  w.rows = 0;
+  w.order.resize((size_t)T);
+  for (int t = 0; t < T; ++t) w.order[(size_t)t] = t;
+  auto kind_of = [](int64_t) { return 0; };
+
+  // sequences whose prefix is shared within the batch
+  std::vector<int> users((size_t)b.n_domains, 0);
+  auto shares = [&](int s) {
+    return b.domain && b.domain[s] >= 0 && b.prefix_len[b.domain[s]] > 0 && b.q_len[s] > 0 &&
+           (int64_t)b.q_len[s] * gs < kOwnRows;
+  };
+  for (int s = 0; s < b.n_seqs; ++s)
+    if (shares(s)) users[(size_t)b.domain[s]]++;
+  std::vector<AttTile> tiles;
+  // each token's tile and first row in it: its own, and its prefix' where shared
+  std::vector<int32_t> tok_tile((size_t)T, -1), tok_pre((size_t)T, -1), tok_r0((size_t)T), pre_r0((size_t)T);
+  auto cut_set = [&](int first, int n_tok, int pos, int pre_ref, int pre_len, int own_ref, std::vector<int32_t>& of,
+                     std::vector<int32_t>& r0) {
+    int kind = kind_of((int64_t)n_tok * gs);
+    while (kRowTiles[kind] < gs) ++kind;
+    const int per = kRowTiles[kind] / gs;
+    for (int t = 0; t < n_tok; t += per) {
+      AttTile x{};
+      x.n_tok = std::min(per, n_tok - t);
+      x.it.kind = kind;
+      x.it.n_rows = x.n_tok * gs;
+      x.it.tok0 = first + t;
+      x.it.pos0 = pos == kAllKeys ? kAllKeys : pos + t;
+      x.it.pre_ref = pre_ref;
+      x.it.pre_len = pre_len;
+      x.it.own_ref = own_ref;
+      x.it.own_end = pos == kAllKeys ? 0 : std::max(0, pos + t + x.n_tok);
+      x.units = seq_cdiv(pre_len, kKeyUnit) + seq_cdiv(x.it.own_end, kKeyUnit);
+      for (int j = 0; j < x.n_tok; ++j) {
+        const size_t tok = (size_t)w.order[(size_t)(first + t + j)];
+        of[tok] = (int32_t)tiles.size();
+        r0[tok] = j * gs;
+      }
+      tiles.push_back(x);
+    }
+  };
+  int t0 = 0;
+  std::vector<int> first_tok((size_t)b.n_seqs);
+  for (int s = 0; s < b.n_seqs; ++s) {
+    first_tok[(size_t)s] = t0;
+    const int n = b.q_len[s], d = b.domain ? b.domain[s] : -1;
+    const bool shared = shares(s) && users[(size_t)d] > 1;
+    const bool solo = d >= 0 && !shared;
+    cut_set(t0, n, b.len[s] - n, solo ? b.prefix_off[d] : 0, solo ? b.prefix_len[d] : 0, b.page_off[s], tok_tile,
+            tok_r0);
+    t0 += n;
+  }
+  for (int d = 0; d < b.n_domains; ++d) {
+    if (users[(size_t)d] < 2) continue;
+    const int first = (int)w.order.size();
+    for (int s = 0; s < b.n_seqs; ++s)
+      if (b.domain[s] == d && shares(s))
+        for (int j = 0; j < b.q_len[s]; ++j) w.order.push_back(first_tok[(size_t)s] + j);
+    cut_set(first, (int)w.order.size() - first, kAllKeys, b.prefix_off[d], b.prefix_len[d], 0, tok_pre,
+            pre_r0);
+  }
+
+  // pieces: enough work items to fill the device, none of less than two units (16 rows)
+  // or four; where the extra partial rows would pass kExtraRows, longer ones
+  int64_t sum[2] = {0, 0};
+  for (const AttTile& x : tiles) sum[x.it.kind != 0] += x.units;
+  int run[2];
+  run[0] = (int)std::max<int64_t>(2, sum[0] * kv_heads / ((int64_t)n_cu * 4));
+  run[1] = (int)std::max<int64_t>(4, sum[1] * kv_heads / ((int64_t)n_cu * 2));
+  for (;;) {
+    int64_t extra = 0;
+    for (const AttTile& x : tiles)
+      extra += (int64_t)std::max(0, seq_cdiv(x.units, run[x.it.kind != 0]) - 1) * x.it.n_rows * kv_heads;
+    if (extra <= kExtraRows) break;
+    run[0] *= 2;
+    run[1] *= 2;
+  }
+  std::vector<int32_t> n_piece(tiles.size()), row_of(tiles.size(), -1);
+  for (size_t i = 0; i < tiles.size(); ++i)
+    n_piece[i] = std::max(1, seq_cdiv(tiles[i].units, run[tiles[i].it.kind != 0]));
+  // a tile is finished in its one item unless its tokens have others
+  std::vector<uint8_t> joined(tiles.size(), 0);
+  for (int t = 0; t < T; ++t) {
+    const int a = tok_tile[(size_t)t], p = tok_pre[(size_t)t];
+    if (p >= 0) joined[(size_t)a] = joined[(size_t)p] = 1;
+    else if (n_piece[(size_t)a] > 1) joined[(size_t)a] = 1;
+  }
+  for (size_t i = 0; i < tiles.size(); ++i) {
+    AttTile& x = tiles[i];
+    if (joined[i]) {
+      row_of[i] = (int32_t)w.rows;
+      w.rows += (int64_t)n_piece[i] * kv_heads * x.it.n_rows;
+    }
+    for (int p = 0; p < n_piece[i]; ++p) {
+      AttItem it = x.it;
+      it.unit0 = (int)((int64_t)x.units * p / n_piece[i]);
+      it.unit1 = (int)((int64_t)x.units * (p + 1) / n_piece[i]);
+      it.out_row = joined[i] ? row_of[i] + p * kv_heads * it.n_rows : -1;
+      w.items.push_back(it);
+    }
+  }
+  std::stable_sort(w.items.begin(), w.items.end(), [](const AttItem& a, const AttItem& c) {
+    return a.kind != c.kind ? a.kind < c.kind : a.unit1 - a.unit0 > c.unit1 - c.unit0;
+  });
+  w.n_kind[0] = w.n_kind[1] = w.n_kind[2] = 0;
+  for (const AttItem& it : w.items) w.n_kind[it.kind]++;
+  for (int t = 0; t < T; ++t) {
+    const int tile[2] = {tok_tile[(size_t)t], tok_pre[(size_t)t]};
+    if (!joined[(size_t)tile[0]]) continue;
+    AttJoin j{};
+    j.tok = t;
+    for (int k = 0; k < 2; ++k) {
+      if (tile[k] < 0) continue;
+      const AttTile& x = tiles[(size_t)tile[k]];
+      j.row[k] = row_of[(size_t)tile[k]];
+      j.n[k] = n_piece[(size_t)tile[k]];
+      j.stride[k] = x.it.n_rows;
+      j.r0[k] = k == 0 ? tok_r0[(size_t)t] : pre_r0[(size_t)t];
+    }
+    w.joins.push_back(j);
+  }
+}
+
+}  // namespace salt

@@ -20,6 +20,8 @@ LIB_PATH = os.path.join(_HERE, "libsalt.so")
 OK, ERR_INVALID_ARG, ERR_OUT_OF_RANGE, ERR_OUT_OF_MEMORY, ERR_NOT_PINNED, ERR_SLOT_EMPTY, \
     ERR_HIP, ERR_BAD_STATE = range(8)
 F32, BF16 = 0, 1
+KV_E4M3, KV_INT8 = 0, 1
+KV_NEW, KV_OWN = 0, 1
 
 # every entry point declared in include/salt.h
 EXPORTS = (
@@ -28,7 +30,9 @@ EXPORTS = (
     "salt_host_alloc", "salt_host_free", "salt_plan_create", "salt_plan_destroy", "salt_plan_set_maps",
     "salt_plan_build", "salt_plan_download", "salt_plan_errors", "salt_plan_tiling", "salt_apply",
     "salt_apply_batch", "salt_apply_batch_noalloc", "salt_apply_batch_timed", "salt_apply_map", "salt_fuse_centroid",
-    "salt_fuse_centroid_timed", "salt_adapter_gram", "salt_route",
+    "salt_fuse_centroid_timed", "salt_adapter_gram", "salt_pin_base", "salt_pin_base_fp8", "salt_read_base",
+    "salt_base_product", "salt_kv_bytes", "salt_kv_create", "salt_kv_destroy", "salt_seqs_create", "salt_seqs_destroy",
+    "salt_seqs_set", "salt_kv_write", "salt_kv_read", "salt_attend", "salt_route",
     "salt_status_str",
     "salt_last_error", "salt_version",
 )
@@ -44,6 +48,18 @@ class Config(C.Structure):
                 ("r_u_max", C.c_int32), ("max_tokens", C.c_int32), ("device", C.c_int32),
                 ("flags", C.c_int32)]
 
+
+
+class KvConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_heads", "n_kv_heads", "head_dim", "page_tokens", "n_pages",
+                                         "format", "flags")]
+
+
+class SeqBatch(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("q_len", C.POINTER(C.c_int32)), ("len", C.POINTER(C.c_int32)),
+                ("page_off", C.POINTER(C.c_int32)), ("pages", C.POINTER(C.c_int32)),
+                ("domain", C.POINTER(C.c_int32)), ("n_domains", C.c_int32), ("prefix_len", C.POINTER(C.c_int32)),
+                ("prefix_off", C.POINTER(C.c_int32)), ("prefix_pages", C.POINTER(C.c_int32))]
 
 
 class RouteResult(C.Structure):
@@ -83,6 +99,19 @@ def _load() -> C.CDLL:
         "salt_fuse_centroid": (C.c_int, [P, I32, I32, C.c_float, VP, C.c_int64, VP]),
         "salt_fuse_centroid_timed": (C.c_int, [P, I32, I32, C.c_float, VP, C.c_int64, VP, VP, VP]),
         "salt_adapter_gram": (C.c_int, [P, VP, I32, VP, I32, C.POINTER(C.c_double), VP]),
+        "salt_pin_base": (C.c_int, [P, I32, VP, C.c_int64, VP]),
+        "salt_pin_base_fp8": (C.c_int, [P, I32, VP, C.c_int64, VP, VP]),
+        "salt_read_base": (C.c_int, [P, I32, VP, C.c_int64, VP]),
+        "salt_base_product": (C.c_int, [P, I32, IP, I32, VP, C.POINTER(VP), VP]),
+        "salt_kv_bytes": (SZ, [C.POINTER(KvConfig)]),
+        "salt_kv_create": (C.c_int, [P, C.POINTER(KvConfig), C.POINTER(P)]),
+        "salt_kv_destroy": (None, [P, P]),
+        "salt_seqs_create": (C.c_int, [P, P, I32, I32, I32, C.POINTER(P)]),
+        "salt_seqs_destroy": (None, [P, P]),
+        "salt_seqs_set": (C.c_int, [P, P, C.POINTER(SeqBatch), VP]),
+        "salt_kv_write": (C.c_int, [P, P, I32, VP, C.c_int64, VP, C.c_int64, VP]),
+        "salt_kv_read": (C.c_int, [P, P, I32, I32, VP, C.c_int64, VP, C.c_int64, VP]),
+        "salt_attend": (C.c_int, [P, P, I32, VP, C.c_int64, VP, C.c_int64, C.c_float, VP]),
         "salt_route": (C.c_int, [I32] + [C.POINTER(C.c_double)] * 5 + [C.c_double, C.c_double] +
                        [C.POINTER(C.c_double)] * 2 + [C.POINTER(RouteResult)]),
         "salt_status_str": (C.c_char_p, [C.c_int]),
@@ -321,6 +350,28 @@ class Context:
         return lib.salt_adapter_gram(self.h, blob1_ptr, r1, blob2_ptr, r2,
                                      out.ctypes.data_as(C.POINTER(C.c_double)), stream)
 
+    def pin_base(self, table: int, w_ptr: int, ldw: int, stream: int = 0):
+        """Quantise the base weight at w_ptr ([in][ldw], device) into the context (8-bit floats, blocks of 128)."""
+        self._check(lib.salt_pin_base(self.h, table, w_ptr, ldw, stream), "salt_pin_base")
+
+    def pin_base_fp8(self, table: int, wq_ptr: int, ldq: int, scales_ptr: int, stream: int = 0):
+        """The base weight from e4m3 codes [out][ldq] and fp32 scales [ceil(out/128)][ceil(in/128)] (device)."""
+        self._check(lib.salt_pin_base_fp8(self.h, table, wq_ptr, ldq, scales_ptr, stream), "salt_pin_base_fp8")
+
+    def read_base(self, table: int, w_ptr: int, ldw: int, stream: int = 0):
+        """The base weight as it is held into w_ptr ([in][ldw], device, context dtype)."""
+        self._check(lib.salt_read_base(self.h, table, w_ptr, ldw, stream), "salt_read_base")
+
+    def base_product(self, tables: Sequence[int], T: int, x_ptr: int, y_ptrs: Sequence[int], stream: int = 0):
+        """salt_base_product: y_ptrs[i] <- x W_base of tables[i], one x for all."""
+        n = len(tables)
+        self._check(lib.salt_base_product(self.h, n, (C.c_int32 * n)(*tables), T, x_ptr, (C.c_void_p * n)(*y_ptrs),
+                                          stream), "salt_base_product")
+
+    def kv_cache(self, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, page_tokens: int, n_pages: int,
+                 fmt: str = "e4m3") -> "KvCache":
+        return KvCache(self, n_layers, n_heads, n_kv_heads, head_dim, page_tokens, n_pages, fmt)
+
     def fuse_centroid_timed(self, table: int, c: int, gamma: float, w_ptr: int, ldw: int, stream: int,
                             start_event: int, stop_event: int):
         """``fuse_centroid`` whose two HIP events record the kernel's own start and end."""
@@ -388,3 +439,89 @@ class Plan:
         n_seg, n_grp = ns.value, ng.value
         return dict(perm=perm[:T], seg_off=seg_off[:n_seg + 1], seg_c=seg_c[:n_seg],
                     seg_u=seg_u[:n_seg], grp_off=grp_off[:n_grp + 1])
+
+
+class KvCache:
+    """A paged KV cache in 8 bits (salt_kv): ``fmt`` is "e4m3" or "int8"."""
+
+    def __init__(self, ctx: Context, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, page_tokens: int,
+                 n_pages: int, fmt: str = "e4m3"):
+        self.ctx = ctx
+        self.cfg = KvConfig(n_layers, n_heads, n_kv_heads, head_dim, page_tokens, n_pages,
+                            {"e4m3": KV_E4M3, "int8": KV_INT8}[fmt], 0)
+        h = C.c_void_p()
+        ctx._check(lib.salt_kv_create(ctx.h, C.byref(self.cfg), C.byref(h)), "salt_kv_create")
+        self.h = h.value
+
+    @property
+    def nbytes(self) -> int:
+        return int(lib.salt_kv_bytes(C.byref(self.cfg)))
+
+    def seqs(self, max_seqs: int, max_tokens: int, max_pages: int) -> "Seqs":
+        return Seqs(self, max_seqs, max_tokens, max_pages)
+
+    def close(self):
+        if self.h and self.ctx.h:
+            lib.salt_kv_destroy(self.ctx.h, self.h)
+        self.h = None
+
+
+class Seqs:
+    """The sequences of one step (salt_seqs): set once, used by every layer."""
+
+    def __init__(self, kv: KvCache, max_seqs: int, max_tokens: int, max_pages: int):
+        self.kv, self.ctx = kv, kv.ctx
+        h = C.c_void_p()
+        self.ctx._check(lib.salt_seqs_create(self.ctx.h, kv.h, max_seqs, max_tokens, max_pages, C.byref(h)),
+                        "salt_seqs_create")
+        self.h = h.value
+
+    def close(self):
+        if self.h and self.ctx.h and self.kv.h:
+            lib.salt_seqs_destroy(self.ctx.h, self.h)
+        self.h = None
+
+    def set_status(self, q_len, length, page_off, pages, domain=None, prefix_len=None, prefix_off=None,
+                   prefix_pages=None, stream: int = 0) -> int:
+        arrs = [None if a is None else np.ascontiguousarray(a, dtype=np.int32)
+                for a in (q_len, length, page_off, pages, domain, prefix_len, prefix_off, prefix_pages)]
+        n, n_d = len(arrs[0]), 0 if arrs[5] is None else len(arrs[5])
+        for a, want in zip(arrs[1:], (n, n + 1, None, n, None, n_d + 1 if n_d else None, None)):
+            if a is not None and want is not None and len(a) != want:
+                raise SaltError(ERR_INVALID_ARG, f"an array of the batch has {len(a)} entries, not {want}")
+        for off, refs in ((arrs[2], arrs[3]), (arrs[6], arrs[7])):
+            if off is not None and refs is not None and len(off) and len(refs) < off[-1]:
+                raise SaltError(ERR_INVALID_ARG, f"{len(refs)} pages, the offsets name {off[-1]}")
+        p = [_i32p(a) for a in arrs]
+        b = SeqBatch(n, p[0], p[1], p[2], p[3], p[4], n_d, p[5], p[6], p[7])
+        return lib.salt_seqs_set(self.ctx.h, self.h, C.byref(b), stream)
+
+    def set(self, q_len, length, page_off, pages, domain=None, prefix_len=None, prefix_off=None, prefix_pages=None,
+            stream: int = 0):
+        """salt_seqs_set: host arrays of the batch (see ``salt_seq_batch`` in include/salt.h)."""
+        self.ctx._check(self.set_status(q_len, length, page_off, pages, domain, prefix_len, prefix_off, prefix_pages,
+                                        stream), "salt_seqs_set")
+
+    def write_status(self, layer: int, k_ptr: int, v_ptr: int, stream: int = 0, ldk: int = 0, ldv: int = 0) -> int:
+        return lib.salt_kv_write(self.ctx.h, self.h, layer, k_ptr, ldk, v_ptr, ldv, stream)
+
+    def write(self, layer: int, k_ptr: int, v_ptr: int, stream: int = 0, ldk: int = 0, ldv: int = 0):
+        """The step's k and v of `layer` into the cache."""
+        self.ctx._check(self.write_status(layer, k_ptr, v_ptr, stream, ldk, ldv), "salt_kv_write")
+
+    def read_status(self, layer: int, what: str, k_ptr: int, v_ptr: int, stream: int = 0, ldk: int = 0,
+                    ldv: int = 0) -> int:
+        return lib.salt_kv_read(self.ctx.h, self.h, layer, {"new": KV_NEW, "own": KV_OWN}[what], k_ptr, ldk, v_ptr,
+                                ldv, stream)
+
+    def read(self, layer: int, what: str, k_ptr: int, v_ptr: int, stream: int = 0, ldk: int = 0, ldv: int = 0):
+        """Plain k and v of the step's tokens ("new") or of all own tokens ("own")."""
+        self.ctx._check(self.read_status(layer, what, k_ptr, v_ptr, stream, ldk, ldv), "salt_kv_read")
+
+    def attend_status(self, layer: int, q_ptr: int, out_ptr: int, scale: float, stream: int = 0, ldq: int = 0,
+                      ldo: int = 0) -> int:
+        return lib.salt_attend(self.ctx.h, self.h, layer, q_ptr, ldq, out_ptr, ldo, scale, stream)
+
+    def attend(self, layer: int, q_ptr: int, out_ptr: int, scale: float, stream: int = 0, ldq: int = 0, ldo: int = 0):
+        """Attention of the step's tokens over the cache."""
+        self.ctx._check(self.attend_status(layer, q_ptr, out_ptr, scale, stream, ldq, ldo), "salt_attend")
