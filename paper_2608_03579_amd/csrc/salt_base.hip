@@ -55,10 +55,9 @@ struct Codes<uint16_t> {
   i32x8 v;
   __device__ __forceinline__ void set(const i32x8& c) { v = c; }
   // a b^T from zero: lane l receives column (l & 15), rows 4 (l >> 4) .. + 3.
-  // (0x7f is the scale 2^0 of the instruction's own scale operands.)
+  // (Constant zeros for the instruction's own scales select the form without them.)
   static __device__ __forceinline__ f32x4 mma(const Codes& a, const Codes& b) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a.v, b.v, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0x7f7f7f7f, 0,
-                                                            0x7f7f7f7f);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a.v, b.v, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
   }
 };
 template <>
@@ -242,43 +241,284 @@ __device__ __forceinline__ int table_of(const BaseArgs& a, int i) {
   return t;
 }
 
-// One wave: 64 outputs x 64 tokens over all inputs, operands straight from memory.
-template <typename E>
-__global__ void __launch_bounds__(64) k_base_product(BaseArgs a) {
+// acc += p * s, a block of 128 inputs' products times its two scales.
+__device__ __forceinline__ void add_scaled(f32x4& acc, const f32x4& p, float s) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) acc[e] = fmaf(p[e], s, acc[e]);
+}
+
+// Up to 16 tokens, in one launch: a block takes OT (1 or 2) tiles of 16 outputs, its 16 waves the
+// input blocks in turn; each wave quantises the x it multiplies (16 tokens x 128 inputs,
+// read from L2 by every block), and the waves' sums meet in LDS.
+constexpr int kFewWaves = 16;
+template <typename E, int OT>
+__global__ void __launch_bounds__(64 * kFewWaves) k_base_few(BaseArgs a) {
+  __shared__ __attribute__((aligned(16))) f32x4 s_acc[OT][kFewWaves][64];
   const int lane = threadIdx.x & 63, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const BaseTable& tab = a.tab[table_of(a, blockIdx.x)];
-  const int o0 = (blockIdx.x - tab.first) * 64, t0 = blockIdx.y * 64;
-  f32x4 acc[4][4];
+  const int tile = (blockIdx.x - tab.first) * OT;
+  const size_t row = (size_t)a.kb * kBaseTile;
+  const uint8_t* w = tab.w + tile * row;
+  const float* sw = tab.sw + tile / 8;
+  f32x4 acc[OT];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < OT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int kb = wave; kb < a.kb; kb += 2 * kFewWaves) {
+    // two blocks' weights on their way before either is used
+    const bool two = kb + kFewWaves < a.kb;
+    const int kb2 = two ? kb + kFewWaves : kb;
+    i32x8 w0[OT], w1[OT];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int kb = 0; kb < a.kb; ++kb) {
-    Codes<E> w[4], x[4];
+    for (int i = 0; i < OT; ++i) {
+      w0[i] = load_tile(w + i * row + (size_t)kb * kBaseTile, lane);
+      w1[i] = load_tile(w + i * row + (size_t)kb2 * kBaseTile, lane);
+    }
+    const float s0 = sw[(size_t)kb * tab.n_blk], s1 = sw[(size_t)kb2 * tab.n_blk];
+    Codes<E> cw, cx;
+    float sx;
+    cx.set(quantise_x(reinterpret_cast<const E*>(a.x), a.T, a.in, 0, kb, lane, sx));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i].set(load_tile(tab.w + ((size_t)(o0 / 16 + i) * a.kb + kb) * kBaseTile, lane));
+    for (int i = 0; i < OT; ++i) {
+      cw.set(w0[i]);
+      add_scaled(acc[i], Codes<E>::mma(cw, cx), s0 * sx);
+    }
+    if (two) {
+      cx.set(quantise_x(reinterpret_cast<const E*>(a.x), a.T, a.in, 0, kb2, lane, sx));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j].set(load_tile(a.xq + ((size_t)(t0 / 16 + j) * a.kb + kb) * kBaseTile, lane));
-    const float sw = tab.sw[(size_t)kb * tab.n_blk + o0 / kBaseBlock];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float s = sw * a.sx[(size_t)kb * a.T_pad + t0 + 16 * j + (lane & 15)];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x4 p = Codes<E>::mma(w[i], x[j]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(p[e], s, acc[i][j][e]);
+      for (int i = 0; i < OT; ++i) {
+        cw.set(w1[i]);
+        add_scaled(acc[i], Codes<E>::mma(cw, cx), s1 * sx);
       }
     }
   }
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int t = t0 + 16 * j + (lane & 15);
+  for (int i = 0; i < OT; ++i) s_acc[i][wave][lane] = acc[i];
+  __syncthreads();
+  if (wave >= OT) return;
+  f32x4 v = s_acc[wave][0][lane];
 #pragma unroll
-    for (int i = 0; i < 4; i += 2) {
-      const int o = o0 + 16 * i + 8 * g;
-      if (t < a.T && o < tab.out) store8(reinterpret_cast<E*>(tab.y) + (size_t)t * tab.out + o, acc[i][j], acc[i + 1][j]);
+  for (int q = 1; q < kFewWaves; ++q) v += s_acc[wave][q][lane];
+  const int t = lane & 15, o = out_of(tile + wave, 4 * g);
+  if (t < a.T && o < tab.out) {
+    E* y = reinterpret_cast<E*>(tab.y) + (size_t)t * tab.out + o;
+    if constexpr (sizeof(E) == 4) *reinterpret_cast<float4*>(y) = make_float4(v[0], v[1], v[2], v[3]);
+    else *reinterpret_cast<uint2*>(y) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  }
+}
+
+// The products of a block's wave tiles to y: token (lane & 15) of token tile j, outputs
+// 8 (lane >> 4) .. + 7 of the tile pair.
+template <typename E>
+__device__ __forceinline__ void store_pair(const BaseArgs& a, const BaseTable& tab, int t0, int o0, int lane,
+                                           const f32x4& lo, const f32x4& hi) {
+  const int t = t0 + (lane & 15), o = o0 + 8 * (lane >> 4);
+  if (t < a.T && o < tab.out) store8(reinterpret_cast<E*>(tab.y) + (size_t)t * tab.out + o, lo, hi);
+}
+
+// Batches too small to fill the device with whole products: a block takes OT output tiles x
+// TT token tiles, its 8 waves the input blocks in turn, operands straight from L2; the
+// waves' sums meet in LDS, where each wave adds up its share of them.
+constexpr int kSplitWaves = 8;
+constexpr size_t split_lds(int ot, int tt) { return (size_t)kSplitWaves * ot * tt * 1024; }
+template <typename E, int OT, int TT>
+__global__ void __launch_bounds__(64 * kSplitWaves) k_base_split(BaseArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  f32x4* s_acc = reinterpret_cast<f32x4*>(lds);        // [tile pair][wave][2][64]
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const BaseTable& tab = a.tab[table_of(a, blockIdx.x)];
+  const int ot0 = (blockIdx.x - tab.first) * OT, tt0 = blockIdx.y * TT;
+  f32x4 acc[OT][TT];
+#pragma unroll
+  for (int i = 0; i < OT; ++i)
+#pragma unroll
+    for (int j = 0; j < TT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int kb = wave; kb < a.kb; kb += kSplitWaves) {
+    Codes<E> w[OT], x[TT];
+    float s[TT];
+    const float sw = tab.sw[(size_t)kb * tab.n_blk + ot0 / 8];
+#pragma unroll
+    for (int i = 0; i < OT; ++i) w[i].set(load_tile(tab.w + ((size_t)(ot0 + i) * a.kb + kb) * kBaseTile, lane));
+#pragma unroll
+    for (int j = 0; j < TT; ++j) {
+      x[j].set(load_tile(a.xq + ((size_t)(tt0 + j) * a.kb + kb) * kBaseTile, lane));
+      s[j] = a.sx[(size_t)kb * a.T_pad + 16 * (tt0 + j) + (lane & 15)];
     }
+#pragma unroll
+    for (int j = 0; j < TT; ++j)
+#pragma unroll
+      for (int i = 0; i < OT; ++i) add_scaled(acc[i][j], Codes<E>::mma(w[i], x[j]), sw * s[j]);
+  }
+#pragma unroll
+  for (int i = 0; i < OT; ++i)
+#pragma unroll
+    for (int j = 0; j < TT; ++j) s_acc[((((i >> 1) * TT + j) * kSplitWaves + wave) * 2 + (i & 1)) * 64 + lane] = acc[i][j];
+  __syncthreads();
+  for (int p = wave; p < OT / 2 * TT; p += kSplitWaves) {
+    f32x4 lo = s_acc[p * kSplitWaves * 128 + lane], hi = s_acc[p * kSplitWaves * 128 + 64 + lane];
+#pragma unroll
+    for (int q = 1; q < kSplitWaves; ++q) {
+      lo += s_acc[(p * kSplitWaves + q) * 128 + lane];
+      hi += s_acc[(p * kSplitWaves + q) * 128 + 64 + lane];
+    }
+    store_pair<E>(a, tab, 16 * (tt0 + p % TT), 16 * (ot0 + 2 * (p / TT)), lane, lo, hi);
+  }
+}
+
+// Copies from memory to LDS without registers: lane l's 16 (4) bytes of src to dst + 16 l
+// (4 l).  src and dst are uniform, `at` is the lane's offset in src.  In assembly, since
+// the compiler makes every read of LDS behind such a copy wait for all of them: the
+// kernels below read one buffer while the other is filled, and wait for their copies
+// themselves (copies_landed) before the barrier behind which they are read.
+__device__ __forceinline__ uint32_t lds_offset(const void* p) {
+  return (uint32_t)(size_t)(__attribute__((address_space(3))) const void*)p;
+}
+__device__ __forceinline__ void copy_kb(const uint8_t* src, uint32_t dst, uint32_t at) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(at), "s"(src) : "memory");
+}
+__device__ __forceinline__ void copy_words(const float* src, uint32_t dst, uint32_t at) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(dst), "v"(at), "s"(src) : "memory");
+}
+__device__ __forceinline__ void copies_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Large batches: a block takes 16 WO WR outputs x 16 TO TR tokens (WR x TR waves of WO x TO
+// tiles).  The operands of one input block are copied into LDS while the previous one is
+// multiplied: two buffers (of their own, so that the compiler sees that a copy into one
+// need not be waited for by reads of the other), one barrier a block.  Tiles lie in LDS as in
+// memory, so copies and operand reads are both 1 KB in a row without bank conflicts.
+template <typename E, int WO, int TO, int WR, int TR>
+__global__ void __launch_bounds__(64 * WR * TR) k_base_tile(BaseArgs a) {
+  constexpr int NO = WO * WR, NT = TO * TR, kWaves = WR * TR;
+  // a buffer: the output tiles, the token tiles, the tokens' scales, and each wave's outputs' scale 64 times
+  constexpr int kSx = (NO + NT) * kBaseTile, kSw = kSx + 64 * NT, kStage = kSw + 256 * kWaves;
+  __shared__ __attribute__((aligned(16))) uint8_t s_a[kStage], s_b[kStage];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // Blocks go to the 8 XCDs in turn; each XCD takes a run of the items, in which four token tiles
+  // share an output tile's operand while it is in the XCD's L2.
+  const int n_tok = (a.T + 16 * NT - 1) / (16 * NT), n_out = gridDim.x / n_tok;
+  int id = blockIdx.x;
+  if (gridDim.x % 8 == 0) id = (id & 7) * (gridDim.x >> 3) + (id >> 3);
+  const int band = id / (4 * n_out), first = 4 * band, width = min(4, n_tok - first);
+  const int in_band = id - 4 * n_out * band;
+  const int item = in_band / width, tok = first + in_band % width;
+  const BaseTable& tab = a.tab[table_of(a, item)];
+  const int ot0 = (item - tab.first) * NO, tt0 = tok * NT;
+  const int wo = (wave % WR) * WO, wt = (wave / WR) * TO;
+
+  // The wave's half tiles of an input block: every kWaves-th of the outputs', then of the tokens'.
+  constexpr int PW = 2 * NO / kWaves, PX = 2 * NT / kWaves;
+  static_assert(kWaves % 2 == 0 && 2 * NO % kWaves == 0 && 2 * NT % kWaves == 0, "whole half tiles to a wave");
+  const size_t row = (size_t)a.kb * kBaseTile, mine = (wave >> 1) * row + (wave & 1) * 1024;
+  const uint8_t* const src_w = tab.w + ot0 * row + mine;
+  const uint8_t* const src_x = a.xq + tt0 * row + mine;
+  const int part = wave % (NT / 4);
+  const float* const src_sx = a.sx + 16 * tt0 + 64 * part;
+  const float* const src_sw = tab.sw + (ot0 + wo) / 8;
+  const uint32_t at16 = 16 * lane, at4 = 4 * lane;
+  auto copy = [&](int kb, uint8_t* stage) {
+    const uint32_t dst = lds_offset(stage);
+    const uint8_t *pw = src_w + (size_t)kb * kBaseTile, *px = src_x + (size_t)kb * kBaseTile;
+#pragma unroll
+    for (int p = 0; p < PW; ++p) copy_kb(pw + (size_t)(p * kWaves / 2) * row, dst + (p * kWaves + wave) * 1024, at16);
+#pragma unroll
+    for (int p = 0; p < PX; ++p)
+      copy_kb(px + (size_t)(p * kWaves / 2) * row, dst + NO * kBaseTile + (p * kWaves + wave) * 1024, at16);
+    // (no branches here: the step's arithmetic must stay in one block of code)
+    copy_words(src_sx + (size_t)kb * a.T_pad, dst + kSx + 256 * part, at4);
+    copy_words(src_sw + (size_t)kb * tab.n_blk, dst + kSw + 256 * wave, 0);
+  };
+  f32x4 acc[WO][TO];
+#pragma unroll
+  for (int i = 0; i < WO; ++i)
+#pragma unroll
+    for (int j = 0; j < TO; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto scales = [&](const uint8_t* st, float (&s)[TO]) {
+    const float sw = *reinterpret_cast<const float*>(st + kSw + 256 * wave);
+#pragma unroll
+    for (int j = 0; j < TO; ++j) s[j] = sw * *reinterpret_cast<const float*>(st + kSx + 4 * (16 * (wt + j) + (lane & 15)));
+  };
+  // One input block: x and the first output tile's codes are in registers (x, w), those of the
+  // next block are fetched behind the barrier, while the last two tiles are multiplied.
+  auto step = [&](int kb, uint8_t* cur, const uint8_t* next, const Codes<E>(&x)[TO], const float(&s)[TO],
+                  Codes<E>(&xn)[TO], float(&sn)[TO], Codes<E>& w) {
+    Codes<E> wt_[WO + 1];
+    wt_[0] = w;
+    f32x4 p[3];
+#pragma unroll
+    for (int i = 0; i < WO; ++i) {
+      if (i + 1 < WO) wt_[i + 1].set(load_tile(cur + (wo + i + 1) * kBaseTile, lane));
+      if (i == WO - 2) {
+        // every read of `cur` is done, and the copy into `next` (of this wave, then of all) has landed
+        copies_landed();
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < TO; ++j) xn[j].set(load_tile(next + (NO + wt + j) * kBaseTile, lane));
+        wt_[WO].set(load_tile(next + wo * kBaseTile, lane));
+        scales(next, sn);
+        copy(min(kb + 2, a.kb - 1), cur);                  // (past the end the last block again: no branch, never used)
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int j = 0; j < TO; ++j) {
+        const int n = i * TO + j;                          // products two behind are scaled and added
+        p[n % 3] = Codes<E>::mma(wt_[i], x[j]);
+        if (n >= 2) add_scaled(acc[(n - 2) / TO][(n - 2) % TO], p[(n - 2) % 3], s[(n - 2) % TO]);
+      }
+      if (i + 1 < WO && i != WO - 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+      for (int j = 0; j < TO; ++j) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int n = WO * TO; n < WO * TO + 2; ++n)
+      add_scaled(acc[(n - 2) / TO][(n - 2) % TO], p[(n - 2) % 3], s[(n - 2) % TO]);
+    w = wt_[WO];
+  };
+  copy(0, s_a);
+  copy(min(1, a.kb - 1), s_b);
+  copies_landed();
+  __syncthreads();
+  Codes<E> x0[TO], x1[TO], w0;
+#pragma unroll
+  for (int j = 0; j < TO; ++j) x0[j].set(load_tile(s_a + (NO + wt + j) * kBaseTile, lane));
+  w0.set(load_tile(s_a + wo * kBaseTile, lane));
+  float sc0[TO], sc1[TO];
+  scales(s_a, sc0);
+  int kb = 0;
+  for (; kb + 2 <= a.kb; kb += 2) {
+    step(kb, s_a, s_b, x0, sc0, x1, sc1, w0);
+    step(kb + 1, s_b, s_a, x1, sc1, x0, sc0, w0);
+  }
+  if (kb < a.kb) step(kb, s_a, s_b, x0, sc0, x1, sc1, w0);
+  // y by way of LDS, 16 tokens at a time, so that each is written in runs of 16 WO outputs (64-byte
+  // pieces straight from the lanes: 57 us of a 456 us product of 8192 tokens went into them).
+  // The last copies have landed and the buffers are no longer read; each wave has its own part.
+  copies_landed();
+  __syncthreads();
+  constexpr int kRow = 16 * WO * (int)sizeof(E), kLd = kRow + 16, kLanes = kRow / 16, kRows = 64 / kLanes;
+  static_assert(kWaves / 2 * 16 * kLd <= kStage, "the waves' parts fit the buffers");
+  uint8_t* const mine_y = (wave < kWaves / 2 ? s_a : s_b) + (wave % (kWaves / 2)) * 16 * kLd;
+#pragma unroll
+  for (int j = 0; j < TO; ++j) {
+#pragma unroll
+    for (int i = 0; i < WO; i += 2)
+      store8(reinterpret_cast<E*>(mine_y + (lane & 15) * kLd) + 16 * i + 8 * (lane >> 4), acc[i][j], acc[i + 1][j]);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int o = 16 * (ot0 + wo) + lane % kLanes * (16 / (int)sizeof(E));
+#pragma unroll
+    for (int r = 0; r < 16; r += kRows) {
+      const uint4 v = *reinterpret_cast<const uint4*>(mine_y + (r + lane / kLanes) * kLd + lane % kLanes * 16);
+      const int t = 16 * (tt0 + wt + j) + r + lane / kLanes;
+      if (t < a.T && o < tab.out)
+        __builtin_nontemporal_store((u32x4){v.x, v.y, v.z, v.w},
+                                    reinterpret_cast<u32x4*>(reinterpret_cast<E*>(tab.y) + (size_t)t * tab.out + o));
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 }
 
@@ -301,21 +541,76 @@ hipError_t launch_base_read(const BasePinArgs& a, int bf16, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_base_product(const BaseArgs& args, int bf16, int n_cu, hipStream_t s) {
-  (void)n_cu;
-  BaseArgs a = args;
-  const dim3 qgrid(cdiv(a.T, 16), cdiv(a.kb, 4));
-  if (bf16) hipLaunchKernelGGL(k_base_quantise<uint16_t>, qgrid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(k_base_quantise<float>, qgrid, dim3(256), 0, s, a);
+namespace {
+
+// Work items, table after table: `per` for every `outs` outputs.
+int number_items(BaseArgs& a, int outs, int per = 1) {
   int items = 0;
   for (int i = 0; i < a.n_tables; ++i) {
     a.tab[i].first = items;
-    items += cdiv(a.tab[i].out, 64);
+    items += per * cdiv(a.tab[i].out, outs);
   }
-  const dim3 grid(items, cdiv(a.T, 64));
-  if (bf16) hipLaunchKernelGGL(k_base_product<uint16_t>, grid, dim3(64), 0, s, a);
-  else hipLaunchKernelGGL(k_base_product<float>, grid, dim3(64), 0, s, a);
+  return items;
+}
+
+template <typename E, int OT, int TT>
+hipError_t launch_split(BaseArgs& a, hipStream_t s) {
+  const dim3 grid(number_items(a, 16 * OT), cdiv(a.T, 16 * TT));
+  hipLaunchKernelGGL((k_base_split<E, OT, TT>), grid, dim3(64 * kSplitWaves), split_lds(OT, TT), s, a);
   return hipGetLastError();
+}
+template <typename E, int WO, int TO, int WR, int TR>
+hipError_t launch_tile(BaseArgs& a, hipStream_t s) {
+  const int items = number_items(a, 16 * WO * WR);
+  hipLaunchKernelGGL((k_base_tile<E, WO, TO, WR, TR>), dim3(items * cdiv(a.T, 16 * TO * TR)), dim3(64 * WR * TR),
+                     0, s, a);
+  return hipGetLastError();
+}
+
+// Which kernel: the largest tile whose blocks still fill the device, since a larger one reads
+// less per product.  us of one product (quantised x included), by tile:
+//   outputs x inputs, tokens    256 x 256   128 x 256   128 x 128   64 x 64   32 x 64   32 x 32
+//   16384 x 3072, 1024               57          64          76       136       130       214
+//   16384 x 3072,  512               48          36          41        73        69       110
+//    4096 x 4096, 2048               64          49          54        71        82        95
+//    4096 x 4096,  256               54          35          32        14        16        18
+//    4096 x 4096,  128               51          33          31        12        11        12
+//    4096 x 4096,   64               50          32          30        12        11        10
+// The first three walk all inputs in each block, the others split them over a block's waves.
+template <typename E>
+hipError_t product(BaseArgs& a, int n_cu, hipStream_t s) {
+  auto blocks = [&](int outs, int toks) {
+    int64_t n = 0;
+    for (int i = 0; i < a.n_tables; ++i) n += cdiv(a.tab[i].out, outs);
+    return n * cdiv(a.T, toks);
+  };
+  // Few tokens: no launch ahead of the product's.  28672 x 4096 of one token 25 us in this way and
+  // 36 behind the quantiser, 3072 x 3072 4.6 and 7.5, of 16 tokens 5.8 and 7.7; in fp32, with
+  // twice the x to read in every block, 8 tokens 6.5 and 7.3, 16 tokens 8.7 and 7.6.  Two
+  // output tiles to a block where one each would not run at once (6144 x 4096: 6.0 and 8.3 us).
+  if (a.T <= (sizeof(E) == 2 ? 16 : 8)) {
+    if (blocks(16, 16) <= n_cu)
+      hipLaunchKernelGGL((k_base_few<E, 1>), dim3(number_items(a, 32, 2)), dim3(64 * kFewWaves), 0, s, a);
+    else hipLaunchKernelGGL((k_base_few<E, 2>), dim3(number_items(a, 32)), dim3(64 * kFewWaves), 0, s, a);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL(k_base_quantise<E>, dim3(cdiv(a.T, 16), cdiv(a.kb, 4)), dim3(256), 0, s, a);
+  const int64_t most = (int64_t)n_cu * 7 / 10, some = (int64_t)n_cu * 6 / 10;
+  if constexpr (sizeof(E) == 2) {       // (bf16 operands of fp32 contexts take twice the registers)
+    if (blocks(256, 256) >= most) return launch_tile<E, 8, 4, 2, 4>(a, s);
+    if (blocks(128, 256) >= most) return launch_tile<E, 4, 4, 2, 4>(a, s);
+  }
+  if (blocks(128, 128) >= most) return launch_tile<E, 4, 4, 2, 2>(a, s);
+  if (blocks(64, 64) >= some) return launch_split<E, 4, 4>(a, s);
+  if (blocks(32, 64) >= some) return launch_split<E, 2, 4>(a, s);
+  return launch_split<E, 2, 2>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_base_product(const BaseArgs& args, int bf16, int n_cu, hipStream_t s) {
+  BaseArgs a = args;
+  return bf16 ? product<uint16_t>(a, n_cu, s) : product<float>(a, n_cu, s);
 }
 
 }  // namespace salt
