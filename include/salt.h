@@ -397,7 +397,7 @@ SALT_API salt_status salt_base_product(salt_ctx* ctx, int32_t n, const int32_t* 
 typedef enum { SALT_KV_E4M3 = 0, SALT_KV_INT8 = 1 } salt_kv_format;
 typedef struct {
   int32_t n_layers;          /* in [1, 1024]                                              */
-  int32_t n_heads;           /* query heads: 1 to 16 times n_kv_heads; query head h reads
+  int32_t n_heads;           /* query heads: 1 to 64 times n_kv_heads; query head h reads
                                 kv head h / (n_heads / n_kv_heads)                          */
   int32_t n_kv_heads;        /* in [1, 256]                                               */
   int32_t head_dim;          /* 64, 128 or 256                                            */

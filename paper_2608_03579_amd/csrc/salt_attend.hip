@@ -14,6 +14,7 @@
 // result's own rounding where a row has few keys); in fp32 contexts both enter in three, 24 bits.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "salt_device.h"
@@ -91,14 +92,40 @@ __device__ __forceinline__ void split_terms(const float (&x)[8], uint4 (&o)[NT])
   }
 }
 
-// The widest of a lane's four: lanes l, l ^ 16, l ^ 32, l ^ 48 hold one row.
+// Over the four lanes of a row (l, l ^ 16, l ^ 32, l ^ 48): halves and then rows of 16 lanes
+// change places, without LDS.
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+// (the instructions themselves: fmaxf first quiets operands that might be signalling NaNs)
+__device__ __forceinline__ float max2(float a, float b) {
+  return __builtin_amdgcn_fmed3f(a, b, __builtin_inff());
+}
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 __device__ __forceinline__ float row_max(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16));
-  return fmaxf(v, __shfl_xor(v, 32));
+  u32x2 w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+  w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
 }
 __device__ __forceinline__ float row_sum(float v) {
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
+  u32x2 w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+  w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(w[0]) + __uint_as_float(w[1]);
+}
+// The running maximum follows a row's largest logit only when that is this much above it
+// (log2): exponentials stay below 2^8, and sums and products are seldom scaled anew.
+constexpr float kMaxSlack = 8.f;
+
+// Word i of p, for a wave-uniform i: by way of the scalar unit.  (p is not written by this launch.)
+__device__ __forceinline__ int uniform_word(const int32_t* p, int i) {
+  return ((const __attribute__((address_space(4))) int32_t*)(uintptr_t)p)[__builtin_amdgcn_readfirstlane(i)];
+}
+
+// A lane's offset from a uniform base, kept as such: otherwise the compiler adds it to the loop's fixed part
+// of the base ahead of the loop, two registers for every load in it.
+__device__ __forceinline__ uint32_t lane_offset(uint32_t v) {
+  asm volatile("" : "+v"(v));
+  return v;
 }
 
 // What a lane holds of 32 keys: k of keys (l & 15) and 16 + (l & 15), dim / 4 values
@@ -126,13 +153,16 @@ __device__ __forceinline__ void load_keys(const AttArgs& a, const AttItem& it, i
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     const int j = min(x.j0 + 16 * t, last & ~15);         // a run of 16 keys lies in one page
-    const int page = a.pages[ref + (j >> lp)];
+    const int page = uniform_word(a.pages, ref + (j >> lp));
+    // (a uniform base and the lane's own offset)
     const size_t vec = (((size_t)page * a.kv.kv_heads + kvh) << lp) + (j & ((1 << lp) - 1));
-    load_words<D / 16>(a.kv.k + vec * D + r * D + g * (D / 4), x.k[t]);
+    const uint8_t *kb = a.kv.k + vec * D, *vb = a.kv.v + vec * D;
+    load_words<D / 16>(kb + lane_offset(r * D + g * (D / 4)), x.k[t]);
+    const uint32_t vo = lane_offset(4 * g * D + r * (D / 16));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) load_words<D / 64>(a.kv.v + vec * D + (4 * g + i) * D + r * (D / 16), x.v[4 * t + i]);
-    const float4 s = *reinterpret_cast<const float4*>(a.kv.ks + vec + 4 * g);
-    const float4 u = *reinterpret_cast<const float4*>(a.kv.vs + vec + 4 * g);
+    for (int i = 0; i < 4; ++i) load_words<D / 64>(vb + vo + i * D, x.v[4 * t + i]);
+    const float4 s = *reinterpret_cast<const float4*>(a.kv.ks + vec + (uint32_t)(4 * g));
+    const float4 u = *reinterpret_cast<const float4*>(a.kv.vs + vec + (uint32_t)(4 * g));
     x.ks[4 * t] = s.x; x.ks[4 * t + 1] = s.y; x.ks[4 * t + 2] = s.z; x.ks[4 * t + 3] = s.w;
     x.vs[4 * t] = u.x; x.vs[4 * t + 1] = u.y; x.vs[4 * t + 2] = u.z; x.vs[4 * t + 3] = u.w;
   }
@@ -184,8 +214,9 @@ __device__ __forceinline__ void use_keys(Rows<E, D>& w, Keys<D>& x, float c, int
     }
   }
   float top = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
-  const float m = fmaxf(w.m, row_max(top));
-  if (__any(m > w.m)) {
+  top = row_max(top);
+  if (__any(top > w.m + kMaxSlack)) {
+    const float m = fmaxf(w.m, top);
     const float alpha = m == kNegInf ? 1.f : __builtin_amdgcn_exp2f(w.m - m);
     w.l *= alpha;
 #pragma unroll
@@ -228,16 +259,20 @@ __device__ __forceinline__ void load8(const E* p, float (&v)[8]) { Ops<E>::to_f3
 
 // One item of up to 16 rows: the block's four waves take 32 keys in turn, and their
 // results are joined in LDS.
+template <int D>
+struct FewLds {
+  float o[4][16][D + 4];
+  float m[4][16], l[4][16];
+};
 template <typename E, int D, int FMT>
-__global__ void __launch_bounds__(256) k_attend_few(AttArgs a) {
+__device__ __forceinline__ void attend_few(const AttArgs& a, const AttItem& it, int kvh, char* lds) {
   using R = Rows<E, D>;
-  constexpr int LD = D + 4;
-  __shared__ __attribute__((aligned(16))) float s_o[4][16][LD];
-  __shared__ float s_m[4][16], s_l[4][16];
+  FewLds<D>& sh = *reinterpret_cast<FewLds<D>*>(lds);
+  auto& s_o = sh.o;
+  auto& s_m = sh.m;
+  auto& s_l = sh.l;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, r = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int kvh = blockIdx.x % a.kv.kv_heads;
-  const AttItem& it = a.items[blockIdx.x / a.kv.kv_heads];
   const int n_pre = 2 * ((it.pre_len + kKeyUnit - 1) / kKeyUnit);
 
   R w;
@@ -327,36 +362,367 @@ __global__ void __launch_bounds__(256) k_attend_few(AttArgs a) {
   if ((tid & 15) == 0) *reinterpret_cast<float2*>(a.stat + 2 * pr) = make_float2(m, l);
 }
 
-// The pieces of a row: 16 lanes per (token, query head).
+// One item of up to 64 RT rows (RT row tiles of 16 to each of four waves), 64 keys at a time: the
+// block takes the keys' codes to bf16 once, into LDS in operand order, two buffers, while
+// it multiplies the ones before.  Power-of-two scales (e4m3) go into the bf16 values,
+// where they are exact; int8's multiply logits and probabilities.  Bound by the vector
+// units: per 64 keys and 32 rows a wave has 1024 cycles of matrix instructions and as
+// many of exponentials, maxima and conversions.
+template <int D>
+struct Staged {            // what a lane brings of its wave's 16 keys
+  uint32_t k[D / 16];      // key (l & 15): dim / 4 values from dim / 4 (l >> 4) on
+  uint32_t v[4][D / 64];   // keys 4 (l >> 4) + i: dim / 16 values from dim / 16 (l & 15) on
+  float ks, vs[4];         // their scales
+  int last;                // the wave's keys past this one are not there
+};
+
+template <typename E, int D, int FMT, int RT>
+struct Many {
+  static constexpr int NT = sizeof(E) == 4 ? 3 : 1;                        // bf16 terms of q and
+  static constexpr int NP = sizeof(E) == 4 ? 3 : 2;                        // of the probabilities
+  static constexpr bool kFold = FMT == kKvE4m3;
+  static constexpr int KS = D / 32, DT = D / 16;
+  static constexpr int kK = 4 * KS * 1024, kBuf = kK + 2 * DT * 1024 + 512;   // a buffer: k, v, 64 scales of each
+};
+
+template <typename E, int D, int FMT, int RT>
+__device__ __forceinline__ void attend_many(const AttArgs& a, const AttItem& it, int kvh, char* lds) {
+  using M = Many<E, D, FMT, RT>;
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n_pre = (it.pre_len + kKeyUnit - 1) / kKeyUnit;
+  const int lp = a.kv.log2_page;
+
+  // a unit's holder: its keys [j0, end), the own ones or the prefix'
+  auto unit = [&](int u, int& j0, int& end) {
+    const bool own = u >= n_pre;
+    j0 = kKeyUnit * (own ? u - n_pre : u);
+    end = own ? it.own_end : it.pre_len;
+    return own;
+  };
+  auto fetch = [&](int u, Staged<D>& x) {
+    int j0, end;
+    const bool own = unit(u, j0, end);
+    const int jw = j0 + 16 * wave, j = min(jw, max(end - 1, 0) & ~15);     // (16 keys lie in one page)
+    const int page = uniform_word(a.pages, (own ? it.own_ref : it.pre_ref) + (j >> lp));
+    const size_t vec = (((size_t)page * a.kv.kv_heads + kvh) << lp) + (j & ((1 << lp) - 1));
+    const uint8_t *kb = a.kv.k + vec * D, *vb = a.kv.v + vec * D;
+    load_words<D / 16>(kb + lane_offset(r * D + g * (D / 4)), x.k);
+    const uint32_t vo = lane_offset(4 * g * D + r * (D / 16));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) load_words<D / 64>(vb + vo + i * D, x.v[i]);
+    x.ks = (a.kv.ks + vec)[(uint32_t)r];
+    const float4 s = *reinterpret_cast<const float4*>(a.kv.vs + vec + (uint32_t)(4 * g));
+    x.vs[0] = s.x; x.vs[1] = s.y; x.vs[2] = s.z; x.vs[3] = s.w;
+    x.last = end - 1 - jw;
+  };
+  auto put = [&](const Staged<D>& x, char* buf) {
+    // k: the wave's subtile, one 16-byte piece per step of 32 values
+    const uint32_t nan = x.ks == x.ks ? 0u : 0x7fc07fc0u;
+#pragma unroll
+    for (int ks = 0; ks < M::KS; ++ks) {
+      uint4 w;
+      if constexpr (M::kFold) {
+        w.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x.k[2 * ks], x.ks, false));
+        w.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x.k[2 * ks], x.ks, true));
+        w.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x.k[2 * ks + 1], x.ks, false));
+        w.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x.k[2 * ks + 1], x.ks, true));
+        w = make_uint4(w.x | nan, w.y | nan, w.z | nan, w.w | nan);
+      } else {
+        const uint2 lo = codes_bf16<FMT>(x.k[2 * ks]), hi = codes_bf16<FMT>(x.k[2 * ks + 1]);
+        w = make_uint4(lo.x, lo.y, hi.x, hi.y);
+      }
+      *reinterpret_cast<uint4*>(buf + ((wave * M::KS + ks) * 64 + lane) * 16) = w;
+    }
+    // v: four keys of every value, half a piece (the other half is the neighbour wave's)
+#pragma unroll
+    for (int q = 0; q < D / 64; ++q) {
+      uint32_t lo[4], hi[4];               // values 4 q, 4 q + 1 and 4 q + 2, 4 q + 3 of each key
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool gone = 4 * g + i > x.last;
+        const uint32_t c = gone ? 0u : x.v[i][q];
+        if constexpr (M::kFold) {
+          const float s = x.vs[i] == x.vs[i] && !gone ? x.vs[i] : 1.f;
+          lo[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, s, false));
+          hi[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, s, true));
+        } else {
+          const uint2 w = codes_bf16<FMT>(c);
+          lo[i] = w.x;
+          hi[i] = w.y;
+        }
+      }
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        const uint32_t* w = d < 2 ? lo : hi;
+        const uint32_t sel = (d & 1) ? 0x07060302u : 0x05040100u;
+        *reinterpret_cast<uint2*>(buf + M::kK + (((wave >> 1) * M::DT + 4 * q + d) * 64 + lane) * 16 + (wave & 1) * 8) =
+            make_uint2(__builtin_amdgcn_perm(w[1], w[0], sel), __builtin_amdgcn_perm(w[3], w[2], sel));
+      }
+    }
+    if constexpr (!M::kFold) {
+      float* sc = reinterpret_cast<float*>(buf + M::kBuf - 512) + 16 * wave;
+      if (g == 0) sc[r] = x.ks;
+      if (r == 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[64 + 4 * g + i] = x.vs[i] == x.vs[i] && 4 * g + i <= x.last ? x.vs[i] : 0.f;
+      }
+    }
+  };
+
+  // the wave's rows
+  uint4 q[RT][M::NT][M::KS];
+  f32x4 o[RT][M::DT], sum[RT];
+  float m[RT], l[RT];
+  int lim[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int row = (wave * RT + t) * 16 + r, ti = row / a.group;
+    const bool used = row < it.n_rows;
+    const int tok = used ? a.order[it.tok0 + ti] : 0;
+    const E* p = reinterpret_cast<const E*>(a.q) + (size_t)tok * a.ldq + (size_t)(kvh * a.group + row - ti * a.group) * D +
+                 g * (D / 4);
+#pragma unroll
+    for (int ks = 0; ks < M::KS; ++ks) {
+      float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (used) load8(p + 8 * ks, f);
+      uint4 tm[M::NT];
+      split_terms<M::NT>(f, tm);
+#pragma unroll
+      for (int n = 0; n < M::NT; ++n) q[t][n][ks] = tm[n];
+    }
+#pragma unroll
+    for (int d = 0; d < M::DT; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m[t] = kNegInf;
+    l[t] = 0.f;
+    lim[t] = it.pos0 + ti + 1;
+  }
+  const int min_lim = it.pos0 + 1;
+  const float c = a.scale * kLog2e;
+
+  // kEdge: some row does not see all of the unit's keys.  Away from the edges, rows have 64 keys or
+  // more, and e4m3's probabilities enter in one bf16 term; their sum is then of the rounded
+  // ones, so that the roundings cancel where a row's weight lies on few keys, and taken as a
+  // row of ones in the product, which spares the vector units.
+  // At the edges row tiles are taken one by one: fewer registers.
+  auto use = [&](auto edge_, auto first_, bool own, int j0, int end, const char* buf) {
+    constexpr bool kEdge = decltype(edge_)::value;
+    constexpr int T0 = decltype(first_)::value, T1 = kEdge ? T0 + 1 : RT;
+    constexpr int NP = M::kFold && M::NP == 2 && !kEdge ? 1 : M::NP;
+    const float* sc = reinterpret_cast<const float*>(buf + M::kBuf - 512);
+    f32x4 s[RT][4];
+    __builtin_amdgcn_s_setprio(1);                           // (the other block's wave does its softmax meanwhile)
+#pragma unroll
+    for (int kp = 0; kp < 4; kp += 2) {                      // two tiles of keys at a time: four sums in turn
+#pragma unroll
+      for (int t = T0; t < T1; ++t) s[t][kp] = s[t][kp + 1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < M::KS; ++ks) {
+        uint4 k[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          k[e] = *reinterpret_cast<const uint4*>(buf + (((kp + e) * M::KS + ks) * 64 + lane) * 16);
+#pragma unroll
+        for (int n = 0; n < M::NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int t = T0; t < T1; ++t) s[t][kp + e] = mma_bf16(k[e], q[t][n][ks], s[t][kp + e]);
+      }
+      __builtin_amdgcn_sched_barrier(0);                     // (no further ahead: the registers would spill)
+    }
+    __builtin_amdgcn_s_setprio(0);
+    uint4 p[RT][2][NP];
+#pragma unroll
+    for (int t = T0; t < T1; ++t) {
+      float y[16];
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) {
+        float4 k4 = make_float4(1.f, 1.f, 1.f, 1.f);
+        if constexpr (!M::kFold) k4 = *reinterpret_cast<const float4*>(sc + 16 * kt + 4 * g);
+        const float kf[4] = {k4.x, k4.y, k4.z, k4.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[4 * kt + i] = M::kFold ? s[t][kt][i] : s[t][kt][i] * kf[i];
+      }
+      if constexpr (kEdge) {
+        const int lt = own ? min(lim[t], end) : end;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (j0 + 16 * (e >> 2) + 4 * g + (e & 3) >= lt) y[e] = kNegInf;
+      }
+      float top = max3(y[0], y[1], y[2]);
+#pragma unroll
+      for (int e = 3; e < 15; e += 2) top = max3(top, y[e], y[e + 1]);
+      top = row_max(max2(top, y[15])) * c;                   // (c > 0)
+      // (always, though the maximum seldom grows: behind a branch the sums are kept twice)
+      const float mn = max2(m[t], top), mu = mn == kNegInf ? 0.f : mn;
+      const float alpha = __builtin_amdgcn_exp2f(m[t] - mu);
+      m[t] = mn;
+      l[t] *= alpha;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[t][i] *= alpha;
+#pragma unroll
+      for (int d = 0; d < M::DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[t][d][i] *= alpha;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(y[8 * h + e], c, -mu));
+        if constexpr (NP > 1) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) l[t] += x[e];
+        }
+        if constexpr (!M::kFold) {
+          const float4 v0 = *reinterpret_cast<const float4*>(sc + 64 + 32 * h + 4 * g);
+          const float4 v1 = *reinterpret_cast<const float4*>(sc + 64 + 32 * h + 16 + 4 * g);
+          x[0] *= v0.x; x[1] *= v0.y; x[2] *= v0.z; x[3] *= v0.w;
+          x[4] *= v1.x; x[5] *= v1.y; x[6] *= v1.z; x[7] *= v1.w;
+        }
+        split_terms<NP>(x, p[t][h]);
+        if constexpr (NP == 1)
+          sum[t] = mma_bf16(make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u), p[t][h][0], sum[t]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int d = 0; d < M::DT; ++d) {
+        const uint4 v = *reinterpret_cast<const uint4*>(buf + M::kK + ((h * M::DT + d) * 64 + lane) * 16);
+#pragma unroll
+        for (int t = T0; t < T1; ++t)
+#pragma unroll
+          for (int n = 0; n < NP; ++n) o[t][d] = mma_bf16(v, p[t][h][n], o[t][d]);
+        if (d % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+      }
+    __builtin_amdgcn_s_setprio(0);
+  };
+
+  const int u1 = it.unit1;
+  if (it.unit0 < u1) {
+    Staged<D> x;
+    fetch(it.unit0, x);
+    put(x, lds);
+    fetch(min(it.unit0 + 1, u1 - 1), x);
+    __syncthreads();
+    char *cur = lds, *next = lds + M::kBuf;
+    int u = it.unit0, j0, end;
+    bool own = unit(u, j0, end);
+    // (past the end the last unit again, into a buffer that is not read: no branch around it)
+    auto step = [&](auto edge_) {
+      put(x, next);                                          // (its readers are behind the last barrier)
+      fetch(min(u + 2, u1 - 1), x);
+      use(edge_, std::integral_constant<int, 0>(), own, j0, end, cur);
+      if constexpr (decltype(edge_)::value && RT == 2) use(edge_, std::integral_constant<int, 1>(), own, j0, end, cur);
+      __syncthreads();
+      char* const t = cur;
+      cur = next;
+      next = t;
+      own = unit(++u, j0, end);
+    };
+    while (u < u1) {
+      while (u < u1 && j0 + kKeyUnit <= (own ? min(min_lim, end) : end)) step(std::false_type());
+      if (u < u1) step(std::true_type());
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const float ls = row_sum(l[t]) + sum[t][0];
+    const int row = (int)lane_offset((wave * RT + t) * 16 + r);   // (worked out again, not kept over the loop)
+    if (row >= it.n_rows) continue;
+    if (it.out_row < 0) {
+      const int ti = row / a.group;
+      E* out = reinterpret_cast<E*>(a.out) + (size_t)a.order[it.tok0 + ti] * a.ldo +
+               (size_t)(kvh * a.group + row - ti * a.group) * D;
+      const float inv = ls == 0.f ? 0.f : 1.0f / ls;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int d = 0; d < M::DT; d += 4) {
+          const float w0 = o[t][d][i] * inv, w1 = o[t][d + 1][i] * inv, w2 = o[t][d + 2][i] * inv, w3 = o[t][d + 3][i] * inv;
+          E* at = out + (4 * g + i) * M::DT + d;
+          if constexpr (sizeof(E) == 4) *reinterpret_cast<float4*>(at) = make_float4(w0, w1, w2, w3);
+          else *reinterpret_cast<uint2*>(at) = make_uint2(pack_bf16x2(w0, w1), pack_bf16x2(w2, w3));
+        }
+    } else {
+      const size_t pr = (size_t)it.out_row + (size_t)kvh * it.n_rows + row;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int d = 0; d < M::DT; d += 4)
+          *reinterpret_cast<float4*>(a.part + pr * D + (4 * g + i) * M::DT + d) =
+              make_float4(o[t][d][i], o[t][d + 1][i], o[t][d + 2][i], o[t][d + 3][i]);
+      if (g == 0) *reinterpret_cast<float2*>(a.stat + 2 * pr) = make_float2(m[t], ls);
+    }
+  }
+}
+
+// A work item of any kind: the long ones of many rows come first, those of few rows fill the
+// places between them.
+template <typename E, int D, int FMT>
+__global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend(AttArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int kvh = blockIdx.x % a.kv.kv_heads;
+  const AttItem& it = a.items[blockIdx.x / a.kv.kv_heads];
+  if (it.kind == 0) attend_few<E, D, FMT>(a, it, kvh, lds);
+  else if (it.kind == 1) attend_many<E, D, FMT, 1>(a, it, kvh, lds);
+  else if constexpr (attend_rows(sizeof(E), D) == kRowTiles[2]) attend_many<E, D, FMT, 2>(a, it, kvh, lds);
+}
+
+// The pieces of a row: 16 lanes per (token, query head).  Lane i reads the maximum and sum of
+// pieces i, i + 16, .., so that their weights are known before any of the sums is needed,
+// and the sums' reads do not wait for each other.
 template <typename E, int D>
 __global__ void __launch_bounds__(256) k_attend_join(AttArgs a) {
   constexpr int DT = D / 16;
   const int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-  const int d0 = (threadIdx.x & 15) * DT;
-  if (i >= (int64_t)a.n_joins * a.heads) return;
-  const AttJoin& j = a.joins[i / a.heads];
+  const int lane = threadIdx.x & 15, d0 = lane * DT;
+  if (i >= (int64_t)a.n_joins * a.heads) return;           // (16 lanes leave together)
+  const AttJoin j = a.joins[i / a.heads];
   const int h = (int)(i % a.heads), kvh = h / a.group, hr = h - kvh * a.group;
+  const int n = j.n[0] + j.n[1];
+  auto row_of = [&](int p) {
+    const int k = p >= j.n[0];
+    return (size_t)(k ? j.row[1] : j.row[0]) +
+           (size_t)((k ? p - j.n[0] : p) * a.kv.kv_heads + kvh) * (k ? j.stride[1] : j.stride[0]) +
+           (k ? j.r0[1] : j.r0[0]) + hr;
+  };
   float m = kNegInf, l = 0.f, v[DT] = {};
+  for (int p0 = 0; p0 < n; p0 += 16) {
+    // (a piece without keys has the sum 0)
+    float2 st = make_float2(kNegInf, 0.f);
+    if (p0 + lane < n) st = *reinterpret_cast<const float2*>(a.stat + 2 * row_of(p0 + lane));
+    float top = st.x;
 #pragma unroll
-  for (int k = 0; k < 2; ++k)
-    for (int p = 0; p < j.n[k]; ++p) {
-      const size_t pr = (size_t)j.row[k] + (size_t)(p * a.kv.kv_heads + kvh) * j.stride[k] + j.r0[k] + hr;
-      const float2 s = *reinterpret_cast<const float2*>(a.stat + 2 * pr);
-      float w[DT];
+    for (int x = 1; x < 16; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+    const float mn = fmaxf(m, top);
+    const float f0 = m == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+    // (a maximum of -inf beside a sum that is not 0: NaN throughout, to be kept)
+    const float f1 = st.x == kNegInf ? 1.f : __builtin_amdgcn_exp2f(st.x - mn);
+    float ls = st.y * f1;
+#pragma unroll
+    for (int x = 1; x < 16; x *= 2) ls += __shfl_xor(ls, x);
+    l = l * (m == kNegInf && l == 0.f ? 0.f : m == kNegInf ? 1.f : f0) + ls;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) v[d] *= f0;
+    m = mn;
+    const int top_p = min(16, n - p0);
+#pragma unroll 4
+    for (int p = 0; p < top_p; ++p) {
+      const float f = __shfl(f1, p, 16);
+      const float* w = a.part + row_of(p0 + p) * D + d0;
 #pragma unroll
       for (int d = 0; d < DT; d += 4) {
-        const float4 x = *reinterpret_cast<const float4*>(a.part + pr * D + d0 + d);
-        w[d] = x.x; w[d + 1] = x.y; w[d + 2] = x.z; w[d + 3] = x.w;
+        const float4 x = *reinterpret_cast<const float4*>(w + d);
+        v[d] = fmaf(x.x, f, v[d]); v[d + 1] = fmaf(x.y, f, v[d + 1]);
+        v[d + 2] = fmaf(x.z, f, v[d + 2]); v[d + 3] = fmaf(x.w, f, v[d + 3]);
       }
-      if (s.x == kNegInf && s.y == 0.f) continue;           // no key in this piece
-      const float mn = fmaxf(m, s.x);
-      const float f0 = m == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-      const float f1 = s.x == kNegInf ? 1.f : __builtin_amdgcn_exp2f(s.x - mn);
-      l = l * f0 + s.y * f1;
-#pragma unroll
-      for (int d = 0; d < DT; ++d) v[d] = v[d] * f0 + w[d] * f1;
-      m = mn;
     }
+  }
   E* out = reinterpret_cast<E*>(a.out) + (size_t)j.tok * a.ldo + (size_t)h * D + d0;
   const float inv = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
@@ -371,8 +737,11 @@ __global__ void __launch_bounds__(256) k_attend_join(AttArgs a) {
 
 template <typename E, int D, int FMT>
 void launch_typed(const AttArgs& a, hipStream_t s) {
-  if (a.n_kind[0])
-    hipLaunchKernelGGL((k_attend_few<E, D, FMT>), dim3(a.n_kind[0] * a.kv.kv_heads), dim3(256), 0, s, a);
+  // (LDS for the kinds that are there)
+  const bool many = a.n_kind[1] + a.n_kind[2] > 0;
+  const size_t lds = std::max(a.n_kind[0] ? sizeof(FewLds<D>) : 0, many ? 2 * (size_t)Many<E, D, FMT, 1>::kBuf : 0);
+  const int n = a.n_kind[0] + a.n_kind[1] + a.n_kind[2];
+  hipLaunchKernelGGL((k_attend<E, D, FMT>), dim3(n * a.kv.kv_heads), dim3(256), lds, s, a);
   if (a.n_joins)
     hipLaunchKernelGGL((k_attend_join<E, D>), dim3((unsigned)(((int64_t)a.n_joins * a.heads + 15) / 16)), dim3(256), 0,
                        s, a);

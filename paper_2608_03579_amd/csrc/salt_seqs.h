@@ -19,7 +19,9 @@ namespace salt {
 
 constexpr int kKeyUnit = 64;       // keys of a unit; prefix and own keys start units of their own
 constexpr int kRowTiles[3] = {16, 64, 128};   // rows of a tile, by item kind
-constexpr int kMaxGroup = 16;      // query heads that share a kv head: a token's rows fit a tile
+constexpr int kMaxGroup = 64;      // query heads that share a kv head: a token's rows fit a tile of 64
+// Rows of the largest tile: fp32 operands (three bf16 terms) and wide heads take the registers of the second 64.
+constexpr int attend_rows(int esize, int dim) { return esize == 2 && dim <= 128 ? kRowTiles[2] : kRowTiles[1]; }
 
 struct AttItem {
   int32_t kind;            // rows of the tile: kRowTiles[kind]
@@ -54,7 +56,7 @@ struct SeqBatch {
 };
 
 struct AttWork {
-  std::vector<AttItem> items;  // by kind, the longest first
+  std::vector<AttItem> items;  // by kind, those of most rows first, the longest first
   int n_kind[3];
   std::vector<int32_t> order;  // token order of the shared row sets, behind the identity [0, T)
   std::vector<AttJoin> joins;
@@ -76,15 +78,17 @@ struct AttTile {
 // long key runs): the cut below keeps to it.
 constexpr int64_t kExtraRows = 1 << 16;
 
-// n_cu: compute units.  T: tokens of the batch (sum of q_len).
-inline void cut_attention(const SeqBatch& b, int T, int heads, int kv_heads, int n_cu, AttWork& w) {
+// n_cu: compute units.  T: tokens of the batch (sum of q_len).  max_rows: attend_rows().
+inline void cut_attention(const SeqBatch& b, int T, int heads, int kv_heads, int max_rows, int n_cu, AttWork& w) {
   const int gs = heads / kv_heads;
   w.items.clear();
   w.joins.clear();
   w.rows = 0;
   w.order.resize((size_t)T);
   for (int t = 0; t < T; ++t) w.order[(size_t)t] = t;
-  auto kind_of = [](int64_t) { return 0; };
+  auto kind_of = [&](int64_t rows) {
+    return rows <= kRowTiles[0] ? 0 : (rows <= kRowTiles[1] || max_rows < kRowTiles[2] ? 1 : 2);
+  };
 
   // sequences whose prefix is shared within the batch
   std::vector<int> users((size_t)b.n_domains, 0);
@@ -183,7 +187,7 @@ inline void cut_attention(const SeqBatch& b, int T, int heads, int kv_heads, int
     }
   }
   std::stable_sort(w.items.begin(), w.items.end(), [](const AttItem& a, const AttItem& c) {
-    return a.kind != c.kind ? a.kind < c.kind : a.unit1 - a.unit0 > c.unit1 - c.unit0;
+    return a.kind != c.kind ? a.kind > c.kind : a.unit1 - a.unit0 > c.unit1 - c.unit0;
   });
   w.n_kind[0] = w.n_kind[1] = w.n_kind[2] = 0;
   for (const AttItem& it : w.items) w.n_kind[it.kind]++;

@@ -234,7 +234,7 @@ const char* kv_config_error(const salt_kv_config& c) {
   if (c.n_pages < 1 || c.n_pages > (1 << 23)) return "n_pages not in [1, 2^23]";
   if (c.n_kv_heads < 1 || c.n_kv_heads > 256) return "n_kv_heads not in [1, 256]";
   if (c.n_heads < c.n_kv_heads || c.n_heads % c.n_kv_heads != 0 || c.n_heads / c.n_kv_heads > salt::kMaxGroup)
-    return "n_heads must be 1 to 16 times n_kv_heads";
+    return "n_heads must be 1 to 64 times n_kv_heads";
   return nullptr;
 }
 // Bytes of one layer's k (or v) codes and of its scales.
@@ -583,7 +583,8 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
     std::vector<int32_t> off((size_t)n + 1);
     for (int i = 0; i <= n; ++i) off[(size_t)i] = n > 0 ? pre_refs + b->page_off[i] : 0;
     const salt::SeqBatch sb{n, nd, b->q_len, b->len, off.data(), b->domain, b->prefix_len, b->prefix_off};
-    salt::cut_attention(sb, T, kv->cfg.n_heads, kv->cfg.n_kv_heads, v.n_cu, w);
+    salt::cut_attention(sb, T, kv->cfg.n_heads, kv->cfg.n_kv_heads,
+                        salt::attend_rows(v.bf16 ? 2 : 4, kv->cfg.head_dim), v.n_cu, w);
     const int n_refs = pre_refs + own_refs;
     auto words = [](size_t k) { return round_up(k, 16); };
     const size_t at_page = 0, at_row = words((size_t)n_refs), at_count = at_row + words((size_t)own_refs);

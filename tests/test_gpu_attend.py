@@ -34,7 +34,7 @@ def test_single_tokens(dim, page, dtype, fmt):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (5, 5), (8, 1), (16, 1), (24, 8), (14, 2)])
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (5, 5), (8, 1), (16, 1), (24, 8), (14, 2), (64, 1), (34, 2)])
 def test_head_layouts(heads, kv_heads, dtype):
     _run(f"heads {heads}/{kv_heads} {dtype}", q_len=[1, 3, 2, 1], length=[40, 3, 200, 1], heads=heads,
          kv_heads=kv_heads, dim=64, page=16, dtype=dtype)
