@@ -501,76 +501,64 @@ __device__ __forceinline__ void attend_many(const AttArgs& a, const AttItem& it,
   const int min_lim = it.pos0 + 1;
   const float c = a.scale * kLog2e;
 
-  // kEdge: some row does not see all of the unit's keys.  Away from the edges, rows have 64 keys or
-  // more, and e4m3's probabilities enter in one bf16 term; their sum is then of the rounded
-  // ones, so that the roundings cancel where a row's weight lies on few keys, and taken as a
-  // row of ones in the product, which spares the vector units.
-  // At the edges row tiles are taken one by one: fewer registers.
-  auto use = [&](auto edge_, auto first_, bool own, int j0, int end, const char* buf) {
-    constexpr bool kEdge = decltype(edge_)::value;
-    constexpr int T0 = decltype(first_)::value, T1 = kEdge ? T0 + 1 : RT;
-    constexpr int NP = M::kFold && M::NP == 2 && !kEdge ? 1 : M::NP;
+  // s <- the logits (before their scale) of 64 keys and row tiles [T0, T1).
+  auto logits = [&](auto first_, auto past_, const char* buf, f32x4(&s)[RT][4]) {
+    constexpr int T0 = decltype(first_)::value, T1 = decltype(past_)::value;
     const float* sc = reinterpret_cast<const float*>(buf + M::kBuf - 512);
-    f32x4 s[RT][4];
-    __builtin_amdgcn_s_setprio(1);                           // (the other block's wave does its softmax meanwhile)
 #pragma unroll
-    for (int kp = 0; kp < 4; kp += 2) {                      // two tiles of keys at a time: four sums in turn
+    for (int kt = 0; kt < 4; ++kt) {
 #pragma unroll
-      for (int t = T0; t < T1; ++t) s[t][kp] = s[t][kp + 1] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int t = T0; t < T1; ++t) s[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int ks = 0; ks < M::KS; ++ks) {
-        uint4 k[2];
+        const uint4 k = *reinterpret_cast<const uint4*>(buf + ((kt * M::KS + ks) * 64 + lane) * 16);
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-          k[e] = *reinterpret_cast<const uint4*>(buf + (((kp + e) * M::KS + ks) * 64 + lane) * 16);
+        for (int t = T0; t < T1; ++t)
 #pragma unroll
-        for (int n = 0; n < M::NT; ++n)
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int t = T0; t < T1; ++t) s[t][kp + e] = mma_bf16(k[e], q[t][n][ks], s[t][kp + e]);
+          for (int n = 0; n < M::NT; ++n) s[t][kt] = mma_bf16(k, q[t][n][ks], s[t][kt]);
       }
-      __builtin_amdgcn_sched_barrier(0);                     // (no further ahead: the registers would spill)
+      if constexpr (!M::kFold) {
+        const float4 k4 = *reinterpret_cast<const float4*>(sc + 16 * kt + 4 * g);
+#pragma unroll
+        for (int t = T0; t < T1; ++t) {
+          s[t][kt][0] *= k4.x; s[t][kt][1] *= k4.y; s[t][kt][2] *= k4.z; s[t][kt][3] *= k4.w;
+        }
+      }
+      if (kt & 1) __builtin_amdgcn_sched_barrier(0);         // (no further ahead: the registers would spill)
     }
-    __builtin_amdgcn_s_setprio(0);
+  };
+  auto largest = [&](const f32x4(&s)[4]) {                   // of a row, in the log2 domain (c > 0)
+    float top = max3(s[0][0], s[0][1], s[0][2]);
+#pragma unroll
+    for (int e = 3; e < 15; e += 2) top = max3(top, s[e >> 2][e & 3], s[(e + 1) >> 2][(e + 1) & 3]);
+    return row_max(max2(top, s[3][3])) * c;
+  };
+  // The sums, so far relative to the maximum m[t], relative to a larger one.
+  auto raise = [&](int t, float top) {
+    const float mn = max2(m[t], top);
+    const float alpha = mn == kNegInf ? 1.f : __builtin_amdgcn_exp2f(m[t] - mn);
+    m[t] = mn;
+    l[t] *= alpha;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[t][i] *= alpha;
+#pragma unroll
+    for (int d = 0; d < M::DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[t][d][i] *= alpha;
+  };
+  // The 64 keys' part of the sums.  NP: bf16 terms of the probabilities.
+  auto add = [&](auto np_, auto first_, auto past_, const char* buf, const f32x4(&s)[RT][4]) {
+    constexpr int NP = decltype(np_)::value, T0 = decltype(first_)::value, T1 = decltype(past_)::value;
+    const float* sc = reinterpret_cast<const float*>(buf + M::kBuf - 512);
     uint4 p[RT][2][NP];
 #pragma unroll
     for (int t = T0; t < T1; ++t) {
-      float y[16];
-#pragma unroll
-      for (int kt = 0; kt < 4; ++kt) {
-        float4 k4 = make_float4(1.f, 1.f, 1.f, 1.f);
-        if constexpr (!M::kFold) k4 = *reinterpret_cast<const float4*>(sc + 16 * kt + 4 * g);
-        const float kf[4] = {k4.x, k4.y, k4.z, k4.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[4 * kt + i] = M::kFold ? s[t][kt][i] : s[t][kt][i] * kf[i];
-      }
-      if constexpr (kEdge) {
-        const int lt = own ? min(lim[t], end) : end;
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (j0 + 16 * (e >> 2) + 4 * g + (e & 3) >= lt) y[e] = kNegInf;
-      }
-      float top = max3(y[0], y[1], y[2]);
-#pragma unroll
-      for (int e = 3; e < 15; e += 2) top = max3(top, y[e], y[e + 1]);
-      top = row_max(max2(top, y[15])) * c;                   // (c > 0)
-      // (always, though the maximum seldom grows: behind a branch the sums are kept twice)
-      const float mn = max2(m[t], top), mu = mn == kNegInf ? 0.f : mn;
-      const float alpha = __builtin_amdgcn_exp2f(m[t] - mu);
-      m[t] = mn;
-      l[t] *= alpha;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sum[t][i] *= alpha;
-#pragma unroll
-      for (int d = 0; d < M::DT; ++d)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[t][d][i] *= alpha;
+      const float mu = m[t] == kNegInf ? 0.f : m[t];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(y[8 * h + e], c, -mu));
+        for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(s[t][2 * h + (e >> 2)][e & 3], c, -mu));
         if constexpr (NP > 1) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) l[t] += x[e];
@@ -585,9 +573,8 @@ __device__ __forceinline__ void attend_many(const AttArgs& a, const AttItem& it,
         if constexpr (NP == 1)
           sum[t] = mma_bf16(make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u), p[t][h][0], sum[t]);
       }
-      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_sched_barrier(0x100);                 // (reads of LDS may go ahead)
     }
-    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -599,7 +586,6 @@ __device__ __forceinline__ void attend_many(const AttArgs& a, const AttItem& it,
           for (int n = 0; n < NP; ++n) o[t][d] = mma_bf16(v, p[t][h][n], o[t][d]);
         if (d % 8 == 7) __builtin_amdgcn_sched_barrier(0);
       }
-    __builtin_amdgcn_s_setprio(0);
   };
 
   const int u1 = it.unit1;
@@ -613,20 +599,55 @@ __device__ __forceinline__ void attend_many(const AttArgs& a, const AttItem& it,
     int u = it.unit0, j0, end;
     bool own = unit(u, j0, end);
     // (past the end the last unit again, into a buffer that is not read: no branch around it)
-    auto step = [&](auto edge_) {
+    auto stage = [&] {
       put(x, next);                                          // (its readers are behind the last barrier)
       fetch(min(u + 2, u1 - 1), x);
-      use(edge_, std::integral_constant<int, 0>(), own, j0, end, cur);
-      if constexpr (decltype(edge_)::value && RT == 2) use(edge_, std::integral_constant<int, 1>(), own, j0, end, cur);
+    };
+    auto advance = [&] {
       __syncthreads();
       char* const t = cur;
       cur = next;
       next = t;
       own = unit(++u, j0, end);
     };
+    constexpr std::integral_constant<int, 0> k0{};
+    constexpr std::integral_constant<int, RT> kRT{};
     while (u < u1) {
-      while (u < u1 && j0 + kKeyUnit <= (own ? min(min_lim, end) : end)) step(std::false_type());
-      if (u < u1) step(std::true_type());
+      // Units that every row sees whole and whose logits pass no row's maximum by much.  e4m3's
+      // probabilities enter in one bf16 term here (rows have 64 keys or more); their sum is then
+      // of the rounded ones, so that the roundings cancel where a row's weight lies on few
+      // keys, and taken as a row of ones in the product, which spares the vector units.
+      // A wave that has to raise a maximum leaves the loop (before the unit's barrier) for
+      // the general form below: behind a branch in here the sums would be kept twice.
+      while (u < u1 && j0 + kKeyUnit <= (own ? min(min_lim, end) : end)) {
+        f32x4 s[RT][4];
+        logits(k0, kRT, cur, s);
+        bool low = false;
+#pragma unroll
+        for (int t = 0; t < RT; ++t) low |= largest(s[t]) > m[t] + kMaxSlack;
+        if (__any(low)) break;
+        stage();
+        add(std::integral_constant<int, M::kFold && M::NP == 2 ? 1 : M::NP>(), k0, kRT, cur, s);
+        advance();
+      }
+      if (u >= u1) break;
+      // Any unit, row tile by row tile (fewer registers).
+      stage();
+      auto general = [&](auto t_) {
+        constexpr int t = decltype(t_)::value;
+        constexpr std::integral_constant<int, t + 1> past{};
+        f32x4 s[RT][4];
+        logits(t_, past, cur, s);
+        const int lt = own ? min(lim[t], end) : end;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (j0 + 16 * (e >> 2) + 4 * g + (e & 3) >= lt) s[t][e >> 2][e & 3] = kNegInf;
+        raise(t, largest(s[t]));
+        add(std::integral_constant<int, M::NP>(), t_, past, cur, s);
+      };
+      general(k0);
+      if constexpr (RT == 2) general(std::integral_constant<int, 1>());
+      advance();
     }
   }
 #pragma unroll
@@ -711,15 +732,23 @@ __global__ void __launch_bounds__(256) k_attend_join(AttArgs a) {
     for (int d = 0; d < DT; ++d) v[d] *= f0;
     m = mn;
     const int top_p = min(16, n - p0);
-#pragma unroll 4
-    for (int p = 0; p < top_p; ++p) {
-      const float f = __shfl(f1, p, 16);
-      const float* w = a.part + row_of(p0 + p) * D + d0;
+    for (int p = 0; p < top_p; p += 4) {                    // (four pieces' reads at a time; past the last one with weight 0)
+      float4 x[4][DT / 4];
 #pragma unroll
-      for (int d = 0; d < DT; d += 4) {
-        const float4 x = *reinterpret_cast<const float4*>(w + d);
-        v[d] = fmaf(x.x, f, v[d]); v[d + 1] = fmaf(x.y, f, v[d + 1]);
-        v[d + 2] = fmaf(x.z, f, v[d + 2]); v[d + 3] = fmaf(x.w, f, v[d + 3]);
+      for (int e = 0; e < 4; ++e) {
+        const float* w = a.part + row_of(p0 + min(p + e, top_p - 1)) * D + d0;
+#pragma unroll
+        for (int d = 0; d < DT / 4; ++d) x[e][d] = *reinterpret_cast<const float4*>(w + 4 * d);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float w1 = __shfl(f1, min(p + e, 15), 16), f = p + e < top_p ? w1 : 0.f;
+        if (f == 0.f) continue;                              // (a sum there may not be finite)
+#pragma unroll
+        for (int d = 0; d < DT / 4; ++d) {
+          v[4 * d] = fmaf(x[e][d].x, f, v[4 * d]); v[4 * d + 1] = fmaf(x[e][d].y, f, v[4 * d + 1]);
+          v[4 * d + 2] = fmaf(x[e][d].z, f, v[4 * d + 2]); v[4 * d + 3] = fmaf(x[e][d].w, f, v[4 * d + 3]);
+        }
       }
     }
   }
