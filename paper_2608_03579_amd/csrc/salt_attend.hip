@@ -257,14 +257,47 @@ __device__ __forceinline__ void use_keys(Rows<E, D>& w, Keys<D>& x, float c, int
 template <typename E>
 __device__ __forceinline__ void load8(const E* p, float (&v)[8]) { Ops<E>::to_f32(Ops<E>::load(p), v); }
 
-// One item of up to 16 rows: the block's four waves take 32 keys in turn, and their
-// results are joined in LDS.
+// A row's result from the lane's part of it (row (l & 15) of a row tile): to out, or as a piece's.
+template <typename E, int D>
+__device__ __forceinline__ void finish_row(const AttArgs& a, const AttItem& it, int kvh, int row, int g,
+                                           const f32x4 (&o)[D / 16], float m, float l) {
+  constexpr int DT = D / 16;
+  if (row >= it.n_rows) return;
+  if (it.out_row < 0) {
+    const int ti = row / a.group;
+    E* out = reinterpret_cast<E*>(a.out) + (size_t)a.order[it.tok0 + ti] * a.ldo +
+             (size_t)(kvh * a.group + row - ti * a.group) * D;
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int d = 0; d < DT; d += 4) {
+        const float w0 = o[d][i] * inv, w1 = o[d + 1][i] * inv, w2 = o[d + 2][i] * inv, w3 = o[d + 3][i] * inv;
+        E* at = out + (4 * g + i) * DT + d;
+        if constexpr (sizeof(E) == 4) *reinterpret_cast<float4*>(at) = make_float4(w0, w1, w2, w3);
+        else *reinterpret_cast<uint2*>(at) = make_uint2(pack_bf16x2(w0, w1), pack_bf16x2(w2, w3));
+      }
+  } else {
+    const size_t pr = (size_t)it.out_row + (size_t)kvh * it.n_rows + row;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int d = 0; d < DT; d += 4)
+        *reinterpret_cast<float4*>(a.part + pr * D + (4 * g + i) * DT + d) =
+            make_float4(o[d][i], o[d + 1][i], o[d + 2][i], o[d + 3][i]);
+    if (g == 0) *reinterpret_cast<float2*>(a.stat + 2 * pr) = make_float2(m, l);
+  }
+}
+
+// One item of up to 16 rows, operands straight from memory.  kWaves = 4: the block's waves take 32
+// keys in turn, and their results are joined in LDS.  kWaves = 1: one wave alone (the block's others
+// have items of their own); no join, and its start-up is paid once for all its keys.
 template <int D>
 struct FewLds {
   float o[4][16][D + 4];
   float m[4][16], l[4][16];
 };
-template <typename E, int D, int FMT>
+template <typename E, int D, int FMT, int kWaves>
 __device__ __forceinline__ void attend_few(const AttArgs& a, const AttItem& it, int kvh, char* lds) {
   using R = Rows<E, D>;
   FewLds<D>& sh = *reinterpret_cast<FewLds<D>*>(lds);
@@ -275,6 +308,11 @@ __device__ __forceinline__ void attend_few(const AttArgs& a, const AttItem& it, 
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_pre = 2 * ((it.pre_len + kKeyUnit - 1) / kKeyUnit);
 
+  // the first keys are on their way before the rows are looked up
+  int st = 2 * it.unit0 + (kWaves == 1 ? 0 : wave);
+  const int st1 = 2 * it.unit1;
+  Keys<D> x;
+  if (st < st1) load_keys<D>(a, it, n_pre, st, kvh, lane, x);
   R w;
   const int ti = r / a.group;
   {
@@ -300,13 +338,9 @@ __device__ __forceinline__ void attend_few(const AttArgs& a, const AttItem& it, 
   const int min_lim = it.pos0 + 1;
   const float c = a.scale * kLog2e;
 
-  int st = 2 * it.unit0 + wave;
-  const int st1 = 2 * it.unit1;
   if (st < st1) {
-    Keys<D> x;
-    load_keys<D>(a, it, n_pre, st, kvh, lane, x);
     while (true) {
-      const int next = st + 4;
+      const int next = st + kWaves;
       Keys<D> y;
       if (next < st1) load_keys<D>(a, it, n_pre, next, kvh, lane, y);
       use_keys<E, D, FMT>(w, x, c, min_lim);
@@ -315,8 +349,12 @@ __device__ __forceinline__ void attend_few(const AttArgs& a, const AttItem& it, 
       st = next;
     }
   }
-  // join the waves
   const float lw = row_sum(w.l);
+  if constexpr (kWaves == 1) {
+    finish_row<E, D>(a, it, kvh, r, g, w.o, w.m, lw);
+    return;
+  }
+  // join the waves
   if (g == 0) {
     s_m[wave][r] = w.m;
     s_l[wave][r] = lw;
@@ -470,6 +508,11 @@ __device__ __forceinline__ void attend_many(const AttArgs& a, const AttItem& it,
     }
   };
 
+  // the first unit is on its way before the rows are looked up
+  const int u1 = it.unit1;
+  Staged<D> x;
+  if (it.unit0 < u1) fetch(it.unit0, x);
+
   // the wave's rows
   uint4 q[RT][M::NT][M::KS];
   f32x4 o[RT][M::DT], sum[RT];
@@ -588,10 +631,7 @@ __device__ __forceinline__ void attend_many(const AttArgs& a, const AttItem& it,
       }
   };
 
-  const int u1 = it.unit1;
   if (it.unit0 < u1) {
-    Staged<D> x;
-    fetch(it.unit0, x);
     put(x, lds);
     fetch(min(it.unit0 + 1, u1 - 1), x);
     __syncthreads();
@@ -612,6 +652,12 @@ __device__ __forceinline__ void attend_many(const AttArgs& a, const AttItem& it,
     };
     constexpr std::integral_constant<int, 0> k0{};
     constexpr std::integral_constant<int, RT> kRT{};
+    // a wave without rows only brings its keys
+    if (wave * RT * 16 >= it.n_rows)
+      while (u < u1) {
+        stage();
+        advance();
+      }
     while (u < u1) {
       // Units that every row sees whole and whose logits pass no row's maximum by much.  e4m3's
       // probabilities enter in one bf16 term here (rows have 64 keys or more); their sum is then
@@ -651,35 +697,8 @@ __device__ __forceinline__ void attend_many(const AttArgs& a, const AttItem& it,
     }
   }
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const float ls = row_sum(l[t]) + sum[t][0];
-    const int row = (int)lane_offset((wave * RT + t) * 16 + r);   // (worked out again, not kept over the loop)
-    if (row >= it.n_rows) continue;
-    if (it.out_row < 0) {
-      const int ti = row / a.group;
-      E* out = reinterpret_cast<E*>(a.out) + (size_t)a.order[it.tok0 + ti] * a.ldo +
-               (size_t)(kvh * a.group + row - ti * a.group) * D;
-      const float inv = ls == 0.f ? 0.f : 1.0f / ls;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int d = 0; d < M::DT; d += 4) {
-          const float w0 = o[t][d][i] * inv, w1 = o[t][d + 1][i] * inv, w2 = o[t][d + 2][i] * inv, w3 = o[t][d + 3][i] * inv;
-          E* at = out + (4 * g + i) * M::DT + d;
-          if constexpr (sizeof(E) == 4) *reinterpret_cast<float4*>(at) = make_float4(w0, w1, w2, w3);
-          else *reinterpret_cast<uint2*>(at) = make_uint2(pack_bf16x2(w0, w1), pack_bf16x2(w2, w3));
-        }
-    } else {
-      const size_t pr = (size_t)it.out_row + (size_t)kvh * it.n_rows + row;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int d = 0; d < M::DT; d += 4)
-          *reinterpret_cast<float4*>(a.part + pr * D + (4 * g + i) * M::DT + d) =
-              make_float4(o[t][d][i], o[t][d + 1][i], o[t][d + 2][i], o[t][d + 3][i]);
-      if (g == 0) *reinterpret_cast<float2*>(a.stat + 2 * pr) = make_float2(m[t], ls);
-    }
-  }
+  for (int t = 0; t < RT; ++t)                               // (the row worked out again, not kept over the loop)
+    finish_row<E, D>(a, it, kvh, (int)lane_offset((wave * RT + t) * 16 + r), g, o[t], m[t], row_sum(l[t]) + sum[t][0]);
 }
 
 // A work item of any kind: the long ones of many rows come first, those of few rows fill the
@@ -687,9 +706,17 @@ __device__ __forceinline__ void attend_many(const AttArgs& a, const AttItem& it,
 template <typename E, int D, int FMT>
 __global__ void __launch_bounds__(256, D <= 128 ? 2 : 1) k_attend(AttArgs a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  const int kvh = blockIdx.x % a.kv.kv_heads;
-  const AttItem& it = a.items[blockIdx.x / a.kv.kv_heads];
-  if (it.kind == 0) attend_few<E, D, FMT>(a, it, kvh, lds);
+  const int n_block = a.n_kind[0] + a.n_kind[1] + a.n_kind[2];   // items that take a block
+  int item = blockIdx.x / a.kv.kv_heads, kvh = blockIdx.x % a.kv.kv_heads;
+  if (item >= n_block) {
+    const int w = (blockIdx.x - n_block * a.kv.kv_heads) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    item = n_block + w / a.kv.kv_heads;
+    kvh = w % a.kv.kv_heads;
+    if (item >= n_block + a.n_kind[3]) return;
+  }
+  const AttItem& it = a.items[item];
+  if (it.kind == 3) attend_few<E, D, FMT, 1>(a, it, kvh, lds);
+  else if (it.kind == 0) attend_few<E, D, FMT, 4>(a, it, kvh, lds);
   else if (it.kind == 1) attend_many<E, D, FMT, 1>(a, it, kvh, lds);
   else if constexpr (attend_rows(sizeof(E), D) == kRowTiles[2]) attend_many<E, D, FMT, 2>(a, it, kvh, lds);
 }
@@ -769,8 +796,8 @@ void launch_typed(const AttArgs& a, hipStream_t s) {
   // (LDS for the kinds that are there)
   const bool many = a.n_kind[1] + a.n_kind[2] > 0;
   const size_t lds = std::max(a.n_kind[0] ? sizeof(FewLds<D>) : 0, many ? 2 * (size_t)Many<E, D, FMT, 1>::kBuf : 0);
-  const int n = a.n_kind[0] + a.n_kind[1] + a.n_kind[2];
-  hipLaunchKernelGGL((k_attend<E, D, FMT>), dim3(n * a.kv.kv_heads), dim3(256), lds, s, a);
+  const int blocks = (a.n_kind[0] + a.n_kind[1] + a.n_kind[2]) * a.kv.kv_heads + cdiv(a.n_kind[3] * a.kv.kv_heads, 4);
+  hipLaunchKernelGGL((k_attend<E, D, FMT>), dim3(blocks), dim3(256), lds, s, a);
   if (a.n_joins)
     hipLaunchKernelGGL((k_attend_join<E, D>), dim3((unsigned)(((int64_t)a.n_joins * a.heads + 15) / 16)), dim3(256), 0,
                        s, a);

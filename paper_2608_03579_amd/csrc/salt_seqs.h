@@ -18,7 +18,7 @@
 namespace salt {
 
 constexpr int kKeyUnit = 64;       // keys of a unit; prefix and own keys start units of their own
-constexpr int kRowTiles[3] = {16, 64, 128};   // rows of a tile, by item kind
+constexpr int kRowTiles[4] = {16, 64, 128, 16};   // rows of a tile, by item kind (0: a block each, 3: a wave each)
 constexpr int kMaxGroup = 64;      // query heads that share a kv head: a token's rows fit a tile of 64
 // Rows of the largest tile: fp32 operands (three bf16 terms) and wide heads take the registers of the second 64.
 constexpr int attend_rows(int esize, int dim) { return esize == 2 && dim <= 128 ? kRowTiles[2] : kRowTiles[1]; }
@@ -57,7 +57,7 @@ struct SeqBatch {
 
 struct AttWork {
   std::vector<AttItem> items;  // by kind, those of most rows first, the longest first
-  int n_kind[3];
+  int n_kind[4];
   std::vector<int32_t> order;  // token order of the shared row sets, behind the identity [0, T)
   std::vector<AttJoin> joins;
   int64_t rows;                // partial rows
@@ -104,7 +104,7 @@ inline void cut_attention(const SeqBatch& b, int T, int heads, int kv_heads, int
   auto cut_set = [&](int first, int n_tok, int pos, int pre_ref, int pre_len, int own_ref, std::vector<int32_t>& of,
                      std::vector<int32_t>& r0) {
     int kind = kind_of((int64_t)n_tok * gs);
-    while (kRowTiles[kind] < gs) ++kind;
+    if (kRowTiles[kind] < gs) kind = 1;                      // (gs <= kMaxGroup)
     const int per = kRowTiles[kind] / gs;
     for (int t = 0; t < n_tok; t += per) {
       AttTile x{};
@@ -147,24 +147,33 @@ inline void cut_attention(const SeqBatch& b, int T, int heads, int kv_heads, int
             pre_r0);
   }
 
-  // pieces: enough work items to fill the device, none of less than two units (16 rows)
-  // or four; where the extra partial rows would pass kExtraRows, longer ones
+  // Tiles of few rows take a block of four waves each, which split the keys, or one wave each where
+  // that gives the device enough waves: 256 sequences of 150 keys, 8 kv heads, behind shared
+  // prefixes, 60 us and not 76; four sequences alone, 10 us and not 13.
+  int64_t few = 0;
+  for (const AttTile& x : tiles) few += x.it.kind == 0;
+  if (few * kv_heads >= (int64_t)n_cu * 4)
+    for (AttTile& x : tiles)
+      if (x.it.kind == 0) x.it.kind = 3;
+  // pieces: enough work items to fill the device, none of less than two units (few rows) or four; where the
+  // extra partial rows would pass kExtraRows, longer ones
   int64_t sum[2] = {0, 0};
-  for (const AttTile& x : tiles) sum[x.it.kind != 0] += x.units;
+  auto wide = [](const AttTile& x) { return x.it.kind == 1 || x.it.kind == 2; };
+  for (const AttTile& x : tiles) sum[wide(x)] += x.units;
   int run[2];
   run[0] = (int)std::max<int64_t>(2, sum[0] * kv_heads / ((int64_t)n_cu * 4));
-  run[1] = (int)std::max<int64_t>(4, sum[1] * kv_heads / ((int64_t)n_cu * 2));
+  run[1] = (int)std::max<int64_t>(4, sum[1] * kv_heads / (int64_t)n_cu);
   for (;;) {
     int64_t extra = 0;
     for (const AttTile& x : tiles)
-      extra += (int64_t)std::max(0, seq_cdiv(x.units, run[x.it.kind != 0]) - 1) * x.it.n_rows * kv_heads;
+      extra += (int64_t)std::max(0, seq_cdiv(x.units, run[wide(x)]) - 1) * x.it.n_rows * kv_heads;
     if (extra <= kExtraRows) break;
     run[0] *= 2;
     run[1] *= 2;
   }
   std::vector<int32_t> n_piece(tiles.size()), row_of(tiles.size(), -1);
   for (size_t i = 0; i < tiles.size(); ++i)
-    n_piece[i] = std::max(1, seq_cdiv(tiles[i].units, run[tiles[i].it.kind != 0]));
+    n_piece[i] = std::max(1, seq_cdiv(tiles[i].units, run[wide(tiles[i])]));
   // a tile is finished in its one item unless its tokens have others
   std::vector<uint8_t> joined(tiles.size(), 0);
   for (int t = 0; t < T; ++t) {
@@ -187,9 +196,10 @@ inline void cut_attention(const SeqBatch& b, int T, int heads, int kv_heads, int
     }
   }
   std::stable_sort(w.items.begin(), w.items.end(), [](const AttItem& a, const AttItem& c) {
-    return a.kind != c.kind ? a.kind > c.kind : a.unit1 - a.unit0 > c.unit1 - c.unit0;
+    const int p = a.kind == 3 ? -1 : a.kind, q = c.kind == 3 ? -1 : c.kind;
+    return p != q ? p > q : a.unit1 - a.unit0 > c.unit1 - c.unit0;
   });
-  w.n_kind[0] = w.n_kind[1] = w.n_kind[2] = 0;
+  std::fill(w.n_kind, w.n_kind + 4, 0);
   for (const AttItem& it : w.items) w.n_kind[it.kind]++;
   for (int t = 0; t < T; ++t) {
     const int tile[2] = {tok_tile[(size_t)t], tok_pre[(size_t)t]};

@@ -201,7 +201,7 @@ struct salt_seqs {
   int64_t own_tokens = 0;
   bool clash = false;                 // two of its tokens' pages are one page
   size_t at_page = 0, at_row = 0, at_count = 0, at_slot = 0, at_order = 0, at_item = 0, at_join = 0;
-  int n_kind[3] = {0, 0, 0}, n_joins = 0;
+  int n_kind[4] = {0, 0, 0, 0}, n_joins = 0;
 };
 
 namespace {
@@ -651,7 +651,7 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
     q->at_order = at_order;
     q->at_item = at_item;
     q->at_join = at_join;
-    std::copy(w.n_kind, w.n_kind + 3, q->n_kind);
+    std::copy(w.n_kind, w.n_kind + 4, q->n_kind);
     q->n_joins = (int)w.joins.size();
   } catch (const std::bad_alloc&) {
     return ctx_fail(ctx, SALT_ERR_OUT_OF_MEMORY, "cutting the batch");
@@ -747,7 +747,7 @@ salt_status salt_attend(salt_ctx* ctx, salt_seqs* q, int32_t layer, const void* 
   a.stat = q->stat;
   a.heads = kv->cfg.n_heads;
   a.group = kv->cfg.n_heads / kv->cfg.n_kv_heads;
-  std::copy(q->n_kind, q->n_kind + 3, a.n_kind);
+  std::copy(q->n_kind, q->n_kind + 4, a.n_kind);
   a.n_joins = q->n_joins;
   a.scale = scale;
   SERVE_HIP(ctx, salt::launch_attend(a, cv.bf16, s));

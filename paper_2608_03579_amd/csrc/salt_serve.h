@@ -117,7 +117,7 @@ struct AttArgs {
   float* part;              // [rows][dim] weighted sums of v, and
   float* stat;              // [rows][2] max (log2) and sum, of rows in pieces
   int32_t heads, group;     // query heads, and those of one kv head
-  int32_t n_kind[3];        // items by kind, in this order
+  int32_t n_kind[4];        // items of each kind; kinds 2, 1, 0 (a block each), then 3 (a wave each)
   int32_t n_joins;
   float scale;              // of the logits
 };
