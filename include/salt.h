@@ -380,8 +380,10 @@ SALT_API salt_status salt_read_base(salt_ctx* ctx, int32_t table, void* w, int64
  * 16-byte aligned; x and the ys must not overlap.  ys are written once, not read.
  * 0 <= T <= max_tokens.  Enqueued on `stream`; nothing is allocated, and results are
  * reproducible bit for bit.  The products of a context share its scratch: the library orders them,
- * also across streams.  Errors: SALT_ERR_OUT_OF_RANGE (table, T), SALT_ERR_BAD_STATE (a base
- * weight never pinned), SALT_ERR_INVALID_ARG; nothing is enqueued then. */
+ * also across streams, so the stream of the latest one must stay valid until the next, or until
+ * salt_destroy; recorded into a graph, all go to the one stream.  Errors: SALT_ERR_OUT_OF_RANGE
+ * (table, T), SALT_ERR_BAD_STATE (a base weight never pinned; under capture behind work on
+ * another stream), SALT_ERR_INVALID_ARG; nothing is enqueued then. */
 SALT_API salt_status salt_base_product(salt_ctx* ctx, int32_t n, const int32_t* tables, int32_t T, const void* x,
                                        void* const* ys, void* stream);
 
@@ -422,8 +424,10 @@ SALT_API void salt_kv_destroy(salt_ctx* ctx, salt_kv* kv);
  * its device buffers (page tables, work items, partial results) for up to max_seqs sequences and
  * domains together, max_tokens new tokens and max_pages page references.  Freed by
  * salt_seqs_destroy (which waits for the device), with its cache, or with the context.  Its work,
- * and that of a cache, is ordered by the library across streams; streams that are to run
- * concurrently need objects of their own, and a cache each. */
+ * and that of a cache, is ordered by the library across streams (the stream of the latest call must
+ * stay valid until the next one, or the object's end; work under capture stays on one stream, else
+ * SALT_ERR_BAD_STATE); streams that are to run concurrently need objects of their own, and a cache
+ * each. */
 SALT_API salt_status salt_seqs_create(salt_ctx* ctx, salt_kv* kv, int32_t max_seqs, int32_t max_tokens,
                                       int32_t max_pages, salt_seqs** out);
 SALT_API void salt_seqs_destroy(salt_ctx* ctx, salt_seqs* seqs);
@@ -450,10 +454,10 @@ typedef struct {
   const int32_t* prefix_pages; /* [prefix_off[n_domains]]                                  */
 } salt_seq_batch;
 /* Validates the batch on the host (every length and page), cuts the attention's work and enqueues one
- * copy on `stream`.  Refused on a stream under capture (SALT_ERR_BAD_STATE): a recorded call serves the
- * batch that was set when it was recorded, and is recorded anew for another.  Errors:
- * SALT_ERR_OUT_OF_RANGE (counts, lengths, pages, domains), SALT_ERR_INVALID_ARG; the batch set
- * before stays then. */
+ * copy on `stream`.  Refused on a stream under capture, and for an object whose batch was recorded
+ * into a graph (SALT_ERR_BAD_STATE): the recorded calls serve that batch for good, another one
+ * takes another object and graph.  Errors: SALT_ERR_OUT_OF_RANGE (counts, lengths, pages, domains),
+ * SALT_ERR_INVALID_ARG; the batch set before stays then. */
 SALT_API salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* seqs, const salt_seq_batch* batch, void* stream);
 
 /* Write the step's keys and values of one layer into the cache: row t of k and v is the step's

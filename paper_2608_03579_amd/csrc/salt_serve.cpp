@@ -61,11 +61,19 @@ struct StreamOrder {
     last = s;
     return hipSuccess;
   }
+  // Work under capture cannot be ordered against work outside it.
+  bool refuses(hipStream_t s) const { return used && last != s && (is_capturing(s) || is_capturing(last)); }
   void destroy() {
     if (hop) (void)hipEventDestroy(hop);
     hop = nullptr;
   }
 };
+salt_status enter_stream(salt_ctx* ctx, StreamOrder& o, hipStream_t s) {
+  if (o.refuses(s))
+    return ctx_fail(ctx, SALT_ERR_BAD_STATE, "work under capture on another stream than the object's last work");
+  SERVE_HIP(ctx, o.enter(s));
+  return SALT_OK;
+}
 
 // The base weights of a context: per table codes and scales, and the scratch that the
 // products quantise x into.
@@ -200,6 +208,7 @@ struct salt_seqs {
   int n_refs = 0, n_own_refs = 0;
   int64_t own_tokens = 0;
   bool clash = false;                 // two of its tokens' pages are one page
+  bool recorded = false;              // a graph holds its launches: grid sizes and places in `dev`
   size_t at_page = 0, at_row = 0, at_count = 0, at_slot = 0, at_order = 0, at_item = 0, at_join = 0;
   int n_kind[4] = {0, 0, 0, 0}, n_joins = 0;
 };
@@ -288,9 +297,13 @@ salt_status rows_arg(salt_ctx* ctx, const char* what, const void* p, int64_t& ld
   return SALT_OK;
 }
 // The batch's buffers and the pool, on `s`.
-hipError_t enter(salt_seqs* q, hipStream_t s) {
-  const hipError_t e = q->order.enter(s);
-  return e != hipSuccess ? e : q->kv->order.enter(s);
+salt_status enter(salt_ctx* ctx, salt_seqs* q, hipStream_t s) {
+  if (q->kv->order.refuses(s))
+    return ctx_fail(ctx, SALT_ERR_BAD_STATE, "work under capture on another stream than the cache's last work");
+  salt_status st = enter_stream(ctx, q->order, s);
+  if (st == SALT_OK) st = enter_stream(ctx, q->kv->order, s);
+  if (st == SALT_OK && is_capturing(s)) q->recorded = true;
+  return st;
 }
 
 }  // namespace
@@ -307,7 +320,7 @@ salt_status salt_pin_base(salt_ctx* ctx, int32_t table, const void* w, int64_t l
   st = base_for(ctx, table, v, &b);
   if (st != SALT_OK) return st;
   const hipStream_t s = (hipStream_t)stream;
-  SERVE_HIP(ctx, b->order.enter(s));
+  if ((st = enter_stream(ctx, b->order, s)) != SALT_OK) return st;
   salt::BasePinArgs a{};
   a.w = const_cast<void*>(w);
   a.ld = ldw;
@@ -331,7 +344,7 @@ salt_status salt_pin_base_fp8(salt_ctx* ctx, int32_t table, const void* wq, int6
   st = base_for(ctx, table, v, &b);
   if (st != SALT_OK) return st;
   const hipStream_t s = (hipStream_t)stream;
-  SERVE_HIP(ctx, b->order.enter(s));
+  if ((st = enter_stream(ctx, b->order, s)) != SALT_OK) return st;
   salt::BasePinArgs a{};
   a.q = static_cast<const uint8_t*>(wq);
   a.sq = scales;
@@ -347,15 +360,14 @@ salt_status salt_pin_base_fp8(salt_ctx* ctx, int32_t table, const void* wq, int6
 salt_status salt_read_base(salt_ctx* ctx, int32_t table, void* w, int64_t ldw, void* stream) {
   SERVE_LIVE(ctx);
   const salt::CtxView v = salt::ctx_view(ctx);
-  const salt_status st =
-      pin_args(ctx, table, w, ldw, table >= 0 && table < v.n_tables ? v.tables[table].out_dim : 0, v);
+  salt_status st = pin_args(ctx, table, w, ldw, table >= 0 && table < v.n_tables ? v.tables[table].out_dim : 0, v);
   if (st != SALT_OK) return st;
   Base* b = static_cast<Base*>(salt::ctx_base(ctx));
   if (!b || !b->tab[(size_t)table].pinned)
     return ctx_fail(ctx, SALT_ERR_BAD_STATE, "the base weight of table %d was never pinned", table);
   SERVE_HIP(ctx, hipSetDevice(v.device));
   const hipStream_t s = (hipStream_t)stream;
-  SERVE_HIP(ctx, b->order.enter(s));
+  if ((st = enter_stream(ctx, b->order, s)) != SALT_OK) return st;
   salt::BasePinArgs a{};
   a.w = w;
   a.ld = ldw;
@@ -370,6 +382,7 @@ salt_status salt_base_product(salt_ctx* ctx, int32_t n, const int32_t* tables, i
                               void* const* ys, void* stream) {
   SERVE_LIVE(ctx);
   const salt::CtxView v = salt::ctx_view(ctx);
+  salt_status st;
   if (n < 0 || (n > 0 && (!tables || !ys))) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "null argument");
   if (T < 0 || T > v.max_tokens)
     return ctx_fail(ctx, SALT_ERR_OUT_OF_RANGE, "T = %d not in [0, %d]", T, v.max_tokens);
@@ -390,7 +403,7 @@ salt_status salt_base_product(salt_ctx* ctx, int32_t n, const int32_t* tables, i
   if (!x || !aligned16(x)) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "null or misaligned x");
   SERVE_HIP(ctx, hipSetDevice(v.device));
   const hipStream_t s = (hipStream_t)stream;
-  SERVE_HIP(ctx, b->order.enter(s));
+  if ((st = enter_stream(ctx, b->order, s)) != SALT_OK) return st;
   salt::BaseArgs a{};
   a.x = x;
   a.xq = b->xq;
@@ -490,6 +503,10 @@ salt_status salt_seqs_create(salt_ctx* ctx, salt_kv* kv, int32_t max_seqs, int32
   const size_t items = 2 * T + (size_t)max_seqs + 16 * (size_t)v.n_cu;
   q->words = 3 * (size_t)max_pages + 3 * T + 64 + items * (sizeof(salt::AttItem) / 4) + T * (sizeof(salt::AttJoin) / 4);
   q->part_rows = (int64_t)(2 * T * (size_t)kv->cfg.n_heads) + salt::kExtraRows;
+  if (q->part_rows > INT32_MAX) {
+    free_seqs(q);
+    return ctx_fail(ctx, SALT_ERR_OUT_OF_RANGE, "%d new tokens of %d heads have too many rows", max_tokens, kv->cfg.n_heads);
+  }
   if (hipMalloc((void**)&q->dev, q->words * 4) != hipSuccess ||
       hipMalloc((void**)&q->part, (size_t)q->part_rows * kv->cfg.head_dim * sizeof(float)) != hipSuccess ||
       hipMalloc((void**)&q->stat, (size_t)q->part_rows * 2 * sizeof(float)) != hipSuccess ||
@@ -527,6 +544,8 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
   salt_status st = seqs_of(ctx, q);
   if (st != SALT_OK) return st;
   if (!b) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "null argument");
+  // (replays would read another batch's arrays in the places of this one's)
+  if (q->recorded) return ctx_fail(ctx, SALT_ERR_BAD_STATE, "the batch was recorded into a graph, which keeps it");
   const int n = b->n_seqs, nd = b->n_domains;
   if (n < 0 || nd < 0 || (int64_t)n + nd > q->max_seqs)
     return ctx_fail(ctx, SALT_ERR_OUT_OF_RANGE, "%d sequences and %d domains, at most %d", n, nd, q->max_seqs);
@@ -632,7 +651,7 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
     std::memcpy(d + at_order, w.order.data(), w.order.size() * 4);
     if (!w.items.empty()) std::memcpy(d + at_item, w.items.data(), w.items.size() * sizeof(salt::AttItem));
     if (!w.joins.empty()) std::memcpy(d + at_join, w.joins.data(), w.joins.size() * sizeof(salt::AttJoin));
-    SERVE_HIP(ctx, q->order.enter(s));
+    if ((st = enter_stream(ctx, q->order, s)) != SALT_OK) return st;
     if (total > 0) {
       SERVE_HIP(ctx, hipMemcpyAsync(q->dev, d, total * 4, hipMemcpyHostToDevice, s));
       SERVE_HIP(ctx, hipEventRecord(q->staged[stage], s));
@@ -672,7 +691,7 @@ salt_status salt_kv_write(salt_ctx* ctx, salt_seqs* q, int32_t layer, const void
   const salt::CtxView cv = salt::ctx_view(ctx);
   SERVE_HIP(ctx, hipSetDevice(cv.device));
   const hipStream_t s = (hipStream_t)stream;
-  SERVE_HIP(ctx, enter(q, s));
+  if ((st = enter(ctx, q, s)) != SALT_OK) return st;
   salt::KvWriteArgs a{};
   a.kv = layer_of(kv, layer);
   a.k = k;
@@ -699,7 +718,7 @@ salt_status salt_kv_read(salt_ctx* ctx, salt_seqs* q, int32_t layer, int32_t wha
   const salt::CtxView cv = salt::ctx_view(ctx);
   SERVE_HIP(ctx, hipSetDevice(cv.device));
   const hipStream_t s = (hipStream_t)stream;
-  SERVE_HIP(ctx, enter(q, s));
+  if ((st = enter(ctx, q, s)) != SALT_OK) return st;
   salt::KvReadArgs a{};
   a.kv = layer_of(kv, layer);
   a.k = k;
@@ -732,7 +751,7 @@ salt_status salt_attend(salt_ctx* ctx, salt_seqs* q, int32_t layer, const void* 
   const salt::CtxView cv = salt::ctx_view(ctx);
   SERVE_HIP(ctx, hipSetDevice(cv.device));
   const hipStream_t s = (hipStream_t)stream;
-  SERVE_HIP(ctx, enter(q, s));
+  if ((st = enter(ctx, q, s)) != SALT_OK) return st;
   salt::AttArgs a{};
   a.kv = layer_of(kv, layer);
   a.q = queries;
