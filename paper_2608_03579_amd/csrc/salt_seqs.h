@@ -13,6 +13,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
 #include <vector>
 
 namespace salt {
@@ -65,9 +66,15 @@ struct AttWork {
 
 inline int seq_cdiv(int a, int b) { return (a + b - 1) / b; }
 
-// Rows that a sequence brings alone from which on it keeps its prefix to itself: a
-// tile of its own rows is full then, and sharing would only add a join.
+// Rows that a sequence brings alone from which on it keeps its prefix to itself: a tile of its own rows
+// is full then, and sharing would only add a join.  8 sequences of 256 tokens and 3 heads behind
+// two prefixes of 8192: 307 us, shared 335; of 20 tokens behind 4096 the two are alike (65 us), and below the
+// prefix would be read once per sequence.
 constexpr int kOwnRows = 128;
+
+// Tiles of few rows: units (on average) up to which one wave works faster on a tile than a block,
+// and units up to which a tile stays whole.
+constexpr int kOneWaveUnits = 16, kWholeUnits = 8;
 
 struct AttTile {
   AttItem it;
@@ -103,13 +110,11 @@ inline void cut_attention(const SeqBatch& b, int T, int heads, int kv_heads, int
   std::vector<int32_t> tok_tile((size_t)T, -1), tok_pre((size_t)T, -1), tok_r0((size_t)T), pre_r0((size_t)T);
   auto cut_set = [&](int first, int n_tok, int pos, int pre_ref, int pre_len, int own_ref, std::vector<int32_t>& of,
                      std::vector<int32_t>& r0) {
-    int kind = kind_of((int64_t)n_tok * gs);
-    if (kRowTiles[kind] < gs) kind = 1;                      // (gs <= kMaxGroup)
-    const int per = kRowTiles[kind] / gs;
+    const int per = kRowTiles[kind_of((int64_t)n_tok * gs)] / gs;   // (a token's rows fit a tile of 64)
     for (int t = 0; t < n_tok; t += per) {
       AttTile x{};
       x.n_tok = std::min(per, n_tok - t);
-      x.it.kind = kind;
+      x.it.kind = kind_of((int64_t)x.n_tok * gs);
       x.it.n_rows = x.n_tok * gs;
       x.it.tok0 = first + t;
       x.it.pos0 = pos == kAllKeys ? kAllKeys : pos + t;
@@ -147,33 +152,79 @@ inline void cut_attention(const SeqBatch& b, int T, int heads, int kv_heads, int
             pre_r0);
   }
 
-  // Tiles of few rows take a block of four waves each, which split the keys, or one wave each where
-  // that gives the device enough waves: 256 sequences of 150 keys, 8 kv heads, behind shared
-  // prefixes, 60 us and not 76; four sequences alone, 10 us and not 13.
-  int64_t few = 0;
-  for (const AttTile& x : tiles) few += x.it.kind == 0;
-  if (few * kv_heads >= (int64_t)n_cu * 4)
-    for (AttTile& x : tiles)
-      if (x.it.kind == 0) x.it.kind = 3;
-  // pieces: enough work items to fill the device, none of less than two units (few rows) or four; where the
-  // extra partial rows would pass kExtraRows, longer ones
-  int64_t sum[2] = {0, 0};
+  // Tiles of few rows.  A block of four waves splits its keys between the waves; one wave each
+  // where the keys are few and the tiles many enough to give every SIMD one.  Of single tokens, 8 kv
+  // heads, block and wave: 64 sequences of 150 keys 8.9 and 12.1 us, 128 of 150 18.0 and 13.8, 256 of 600
+  // 82 and 69, 128 of 2000 114 and 129.
   auto wide = [](const AttTile& x) { return x.it.kind == 1 || x.it.kind == 2; };
-  for (const AttTile& x : tiles) sum[wide(x)] += x.units;
-  int run[2];
-  run[0] = (int)std::max<int64_t>(2, sum[0] * kv_heads / ((int64_t)n_cu * 4));
-  run[1] = (int)std::max<int64_t>(4, sum[1] * kv_heads / (int64_t)n_cu);
-  for (;;) {
-    int64_t extra = 0;
-    for (const AttTile& x : tiles)
-      extra += (int64_t)std::max(0, seq_cdiv(x.units, run[wide(x)]) - 1) * x.it.n_rows * kv_heads;
-    if (extra <= kExtraRows) break;
-    run[0] *= 2;
-    run[1] *= 2;
+  int64_t few = 0, few_units = 0;
+  for (const AttTile& x : tiles)
+    if (!wide(x)) ++few, few_units += x.units;
+  const bool one_wave = few * kv_heads >= (int64_t)n_cu * 4 && few_units <= few * kOneWaveUnits;
+  if (one_wave)
+    for (AttTile& x : tiles)
+      if (!wide(x)) x.it.kind = 3;
+  // Their pieces: an item for every compute unit, but no more pieces than the join is worth, which
+  // reads them one after the other: 16384 keys of one sequence take 42 us in pieces of 2 units, 19 of 8, 30 of
+  // 32; 65000 keys 159, 57 and 37.  A join costs 3 us by itself: 150 keys 9.2 us in two pieces, 6.6 in one.
+  const int64_t fill = (few_units * kv_heads + n_cu - 1) / n_cu;
+  auto few_pieces = [&](const AttTile& x, int64_t least) {
+    if (x.units <= kWholeUnits) return 1;
+    const int64_t run = std::max<int64_t>({least, fill, (int64_t)std::ceil(std::sqrt((double)x.units) / 2)});
+    return (int)((x.units + run - 1) / run);
+  };
+  std::vector<int32_t> n_piece(tiles.size(), 1), row_of(tiles.size(), -1);
+  int64_t few_extra = 0;
+  for (int64_t least = 1;; least *= 2) {
+    few_extra = 0;
+    for (size_t i = 0; i < tiles.size(); ++i)
+      if (!wide(tiles[i])) {
+        n_piece[i] = few_pieces(tiles[i], least);
+        few_extra += (int64_t)(n_piece[i] - 1) * tiles[i].it.n_rows * kv_heads;
+      }
+    if (few_extra <= kExtraRows) break;
   }
-  std::vector<int32_t> n_piece(tiles.size()), row_of(tiles.size(), -1);
+  // Tiles of many rows: the longest one in 1 to 16 pieces, the others in pieces as long, whichever
+  // count is estimated to end first.
+  int longest = 0;
+  int64_t units = 0, few_blocks = 0;
+  for (size_t i = 0; i < tiles.size(); ++i) {
+    if (wide(tiles[i])) longest = std::max(longest, tiles[i].units), units += tiles[i].units;
+    else few_blocks += n_piece[i];
+  }
+  // of the tiles of few rows: blocks (of four waves), and their work in units of the others
+  const double few_work = (double)few_units * kv_heads * (one_wave ? 0.25 : 0.2);
+  few_blocks = few_blocks * kv_heads / (one_wave ? 4 : 1);
+  int best_run = std::max(1, longest);
+  double best = 1e300;
+  for (int p = 1, last = 0; p <= 16; ++p) {
+    const int run = std::max(1, seq_cdiv(longest, p));
+    if (p > 1 && (run < 4 || run == last)) continue;
+    last = run;
+    int64_t n = 0, parts = 0, extra = few_extra, part_rows = 0;
+    for (const AttTile& x : tiles)
+      if (wide(x)) {
+        const int k = std::max(1, seq_cdiv(x.units, run));
+        n += (int64_t)k * kv_heads;
+        parts += k - 1;
+        extra += (int64_t)(k - 1) * x.it.n_rows * kv_heads;
+        if (k > 1) part_rows += (int64_t)k * x.it.n_rows * kv_heads;
+      }
+    if (p > 1 && (extra > kExtraRows || parts > (int64_t)n_cu * 8)) break;
+    // In the time of a unit: rounds of two blocks a compute unit, of which one that has it to itself takes
+    // 0.65 of the time, half a unit to begin and end a piece, the longest piece's end alone, and
+    // where rows are joined a launch and 15000 partial rows to the unit.  Measured with 8 kv heads and
+    // groups of 4, whole and in 2, 3 and 4 pieces: 16 x 40 tokens of 2000 keys 73, 57, 71, 71 us; 2048
+    // tokens of 8192 287, 311; 256 tokens of 4096 128, 78, 61, 52.
+    const int64_t blocks = n + few_blocks, full = blocks / (2 * n_cu), rest = blocks % (2 * n_cu);
+    const double rounds = (double)full + (rest == 0 ? 0. : rest <= n_cu ? 0.65 : 1.);
+    const double mean = ((double)units * kv_heads + few_work) / (double)std::max<int64_t>(blocks, 1);
+    const double time = std::max(rounds * (mean + 0.5), 0.65 * run + 0.35 * (blocks > n_cu ? mean : 0.)) +
+                        (part_rows ? 1.5 + (double)part_rows / 15000 : 0.);
+    if (time < best) best = time, best_run = run;
+  }
   for (size_t i = 0; i < tiles.size(); ++i)
-    n_piece[i] = std::max(1, seq_cdiv(tiles[i].units, run[wide(tiles[i])]));
+    if (wide(tiles[i])) n_piece[i] = std::max(1, seq_cdiv(tiles[i].units, best_run));
   // a tile is finished in its one item unless its tokens have others
   std::vector<uint8_t> joined(tiles.size(), 0);
   for (int t = 0; t < T; ++t) {
