@@ -249,7 +249,8 @@ __device__ __forceinline__ void add_scaled(f32x4& acc, const f32x4& p, float s) 
 
 // Up to 16 tokens, in one launch: a block takes OT (1 or 2) tiles of 16 outputs, its 16 waves the
 // input blocks in turn; each wave quantises the x it multiplies (16 tokens x 128 inputs,
-// read from L2 by every block), and the waves' sums meet in LDS.
+// read from L2 by every block), and the waves' sums meet in LDS.  One token: 3072 x 3072 4.5 us, a
+// launch's own time and two memory latencies; 28672 x 4096 25 us, 4.7 TB/s of weights.
 constexpr int kFewWaves = 16;
 template <typename E, int OT>
 __global__ void __launch_bounds__(64 * kFewWaves) k_base_few(BaseArgs a) {
@@ -318,7 +319,8 @@ __device__ __forceinline__ void store_pair(const BaseArgs& a, const BaseTable& t
 
 // Batches too small to fill the device with whole products: a block takes OT output tiles x
 // TT token tiles, its 8 waves the input blocks in turn, operands straight from L2; the
-// waves' sums meet in LDS, where each wave adds up its share of them.
+// waves' sums meet in LDS, where each wave adds up its share of them.  Latency and L2 bound it: 6144
+// x 4096 of 64 tokens 7.8 us (26 MB, 3.4 TB/s), 4096 x 4096 of 256 11 us, and 3 for the quantiser.
 constexpr int kSplitWaves = 8;
 constexpr size_t split_lds(int ot, int tt) { return (size_t)kSplitWaves * ot * tt * 1024; }
 template <typename E, int OT, int TT>
@@ -375,10 +377,10 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p) {
   return (uint32_t)(size_t)(__attribute__((address_space(3))) const void*)p;
 }
 __device__ __forceinline__ void copy_kb(const uint8_t* src, uint32_t dst, uint32_t at) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(at), "s"(src) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(at), "s"(src) : "memory", "m0");
 }
 __device__ __forceinline__ void copy_words(const float* src, uint32_t dst, uint32_t at) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(dst), "v"(at), "s"(src) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(dst), "v"(at), "s"(src) : "memory", "m0");
 }
 __device__ __forceinline__ void copies_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
@@ -387,6 +389,10 @@ __device__ __forceinline__ void copies_landed() { asm volatile("s_waitcnt vmcnt(
 // multiplied: two buffers (of their own, so that the compiler sees that a copy into one
 // need not be waited for by reads of the other), one barrier a block.  Tiles lie in LDS as in
 // memory, so copies and operand reads are both 1 KB in a row without bank conflicts.
+// 16384 x 3072, 8192 tokens: 390 to 437 us from card to card with the quantiser's 14, 1.9 to 2.1
+// PFLOP/s.  399 without y's stores (268 MB, which nothing overlaps), 380 without the copies, 390 without
+// the matrix instructions in a run of 425: no one of them bounds it.  Matrix units busy 56 %; alone they
+// reach 4.7 PFLOP/s here, 4.5 with the four additions that the scales need behind each.
 template <typename E, int WO, int TO, int WR, int TR>
 __global__ void __launch_bounds__(64 * WR * TR) k_base_tile(BaseArgs a) {
   constexpr int NO = WO * WR, NT = TO * TR, kWaves = WR * TR;
@@ -495,8 +501,9 @@ __global__ void __launch_bounds__(64 * WR * TR) k_base_tile(BaseArgs a) {
     step(kb + 1, s_b, s_a, x1, sc1, x0, sc0, w0);
   }
   if (kb < a.kb) step(kb, s_a, s_b, x0, sc0, x1, sc1, w0);
-  // y by way of LDS, 16 tokens at a time, so that each is written in runs of 16 WO outputs (64-byte
-  // pieces straight from the lanes: 57 us of a 456 us product of 8192 tokens went into them).
+  // y by way of LDS, 16 tokens at a time, so that each is written in runs of 16 WO outputs, and past the
+  // caches, which keep x and W: 16384 x 3072, 8192 tokens, 456 us straight from the lanes, 452 by
+  // way of LDS, 437 past the caches as well.
   // The last copies have landed and the buffers are no longer read; each wave has its own part.
   copies_landed();
   __syncthreads();

@@ -1,6 +1,6 @@
 """examples/attention_block.py: base product, apply, cache and attention together, against float64 on unquantised
 values.  Bound: x and the weights each lose up to 2^-4 of a value to e4m3 (an rms of 2.6 % each for values
-spread over a binade), k and v again; four such errors on the way to y add to some 6 %, less where
+spread over a binade), k and v again; such errors on the way to y measure 8.3 % together, less where
 attention averages them out.  A missing adapter, prompt or head would show as 20 % or more."""
 import importlib.util
 import os
