@@ -85,6 +85,9 @@ struct AttTile {
 // Partial rows that a plan of at most T tokens can need beyond two per row (pieces of
 // long key runs): the cut below keeps to it.
 constexpr int64_t kExtraRows = 1 << 16;
+// Items of T tokens at most: two tiles to a token, and a piece beyond a tile's first brings a partial row
+// for every head or more.
+constexpr int64_t attend_max_items(int64_t T, int heads) { return 2 * T + kExtraRows / heads; }
 
 // n_cu: compute units.  T: tokens of the batch (sum of q_len).  max_rows: attend_rows().
 inline void cut_attention(const SeqBatch& b, int T, int heads, int kv_heads, int max_rows, int n_cu, AttWork& w) {

@@ -499,9 +499,9 @@ salt_status salt_seqs_create(salt_ctx* ctx, salt_kv* kv, int32_t max_seqs, int32
   q->max_tokens = max_tokens;
   q->max_pages = max_pages;
   const size_t T = (size_t)max_tokens;
-  // (salt_seqs.h: at most two tiles to a token, and some 4 + 2 pieces to a compute unit beside)
-  const size_t items = 2 * T + (size_t)max_seqs + 16 * (size_t)v.n_cu;
-  q->words = 3 * (size_t)max_pages + 3 * T + 64 + items * (sizeof(salt::AttItem) / 4) + T * (sizeof(salt::AttJoin) / 4);
+  const size_t items = (size_t)salt::attend_max_items(max_tokens, kv->cfg.n_heads);
+  // (each of the six arrays behind the first starts at a multiple of 16 words)
+  q->words = 3 * (size_t)max_pages + 3 * T + 6 * 16 + items * (sizeof(salt::AttItem) / 4) + T * (sizeof(salt::AttJoin) / 4);
   q->part_rows = (int64_t)(2 * T * (size_t)kv->cfg.n_heads) + salt::kExtraRows;
   if (q->part_rows > INT32_MAX) {
     free_seqs(q);
