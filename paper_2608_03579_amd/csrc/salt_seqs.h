@@ -64,6 +64,25 @@ struct AttWork {
   int64_t rows;                // partial rows
 };
 
+// Of page reference `k` (from 0) of a holder of `len` tokens whose first is row `row`: its tokens, and the
+// row of the first of them.  References past the last token have none.
+inline int32_t page_count(int len, int page_tokens, int k) {
+  return (int32_t)std::max<int64_t>(0, std::min<int64_t>(page_tokens, len - (int64_t)k * page_tokens));
+}
+inline int32_t page_row(int row, int len, int page_tokens, int k) {
+  return page_count(len, page_tokens, k) > 0 ? row + k * page_tokens : row;
+}
+
+// Blocks of 256 threads that a launch can have: fewer than 2^32 threads along x.
+constexpr int64_t kMaxBlocks = ((int64_t)1 << 24) - 1;
+// The most blocks of a launch on the batch: its items, joins, new tokens (16 vectors a block) and own pages.
+inline int64_t most_blocks(const AttWork& w, int T, int heads, int kv_heads, int own_refs) {
+  const int64_t items = (int64_t)(w.n_kind[0] + w.n_kind[1] + w.n_kind[2]) * kv_heads +
+                        ((int64_t)w.n_kind[3] * kv_heads + 3) / 4;
+  const int64_t joins = ((int64_t)w.joins.size() * heads + 15) / 16, rows = ((int64_t)T * kv_heads + 15) / 16;
+  return std::max(std::max(items, joins), std::max<int64_t>(rows, own_refs));
+}
+
 inline int seq_cdiv(int a, int b) { return (a + b - 1) / b; }
 
 // Rows that a sequence brings alone from which on it keeps its prefix to itself: a tile of its own rows
@@ -147,12 +166,19 @@ inline void cut_attention(const SeqBatch& b, int T, int heads, int kv_heads, int
             tok_tile, tok_r0);
     t0 += n;
   }
+  // (the sequences by domain, each domain's in order)
+  std::vector<int> user_at((size_t)b.n_domains + 1, 0);
+  for (int d = 0; d < b.n_domains; ++d) user_at[(size_t)d + 1] = user_at[(size_t)d] + users[(size_t)d];
+  std::vector<int> by_domain((size_t)user_at[(size_t)b.n_domains]), next(user_at.begin(), user_at.end() - 1);
+  for (int s = 0; s < b.n_seqs; ++s)
+    if (shares(s)) by_domain[(size_t)next[(size_t)b.domain[s]]++] = s;
   for (int d = 0; d < b.n_domains; ++d) {
     if (users[(size_t)d] < 2) continue;
     const int first = (int)w.order.size();
-    for (int s = 0; s < b.n_seqs; ++s)
-      if (b.domain[s] == d && shares(s))
-        for (int j = 0; j < b.q_len[s]; ++j) w.order.push_back(first_tok[(size_t)s] + j);
+    for (int u = user_at[(size_t)d]; u < user_at[(size_t)d + 1]; ++u) {
+      const int s = by_domain[(size_t)u];
+      for (int j = 0; j < b.q_len[s]; ++j) w.order.push_back(first_tok[(size_t)s] + j);
+    }
     cut_set(first, (int)w.order.size() - first, kAllKeys, b.prefix_off[d], b.prefix_len[d], 0, true, tok_pre,
             pre_r0);
   }

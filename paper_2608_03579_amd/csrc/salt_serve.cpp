@@ -604,6 +604,10 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
     const salt::SeqBatch sb{n, nd, b->q_len, b->len, off.data(), b->domain, b->prefix_len, b->prefix_off};
     salt::cut_attention(sb, T, kv->cfg.n_heads, kv->cfg.n_kv_heads,
                         salt::attend_rows(v.bf16 ? 2 : 4, kv->cfg.head_dim), v.n_cu, w);
+    const int64_t blocks = salt::most_blocks(w, T, kv->cfg.n_heads, kv->cfg.n_kv_heads, own_refs);
+    if (blocks > salt::kMaxBlocks)
+      return ctx_fail(ctx, SALT_ERR_OUT_OF_RANGE, "the batch takes launches of %lld blocks, at most %lld",
+                      (long long)blocks, (long long)salt::kMaxBlocks);
     const int n_refs = pre_refs + own_refs;
     auto words = [](size_t k) { return round_up(k, 16); };
     const size_t at_page = 0, at_row = words((size_t)n_refs), at_count = at_row + words((size_t)own_refs);
@@ -643,8 +647,8 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
       }
       for (int r = b->page_off[i]; r < b->page_off[i + 1]; ++r) {
         const int k = r - b->page_off[i];
-        d[at_row + r] = row + k * pt;
-        d[at_count + r] = std::max(0, std::min(pt, len - k * pt));
+        d[at_row + r] = salt::page_row(row, len, pt, k);
+        d[at_count + r] = salt::page_count(len, pt, k);
       }
       row += len;
     }
