@@ -474,12 +474,17 @@ class Seqs:
         h = C.c_void_p()
         self.ctx._check(lib.salt_seqs_create(self.ctx.h, kv.h, max_seqs, max_tokens, max_pages, C.byref(h)),
                         "salt_seqs_create")
-        self.h = h.value
+        self._h = h.value
+
+    @property
+    def h(self):
+        """The handle; None (which every call refuses) once it, its cache or its context was closed."""
+        return self._h if self.kv.h and self.ctx.h else None
 
     def close(self):
-        if self.h and self.ctx.h and self.kv.h:
+        if self.h:
             lib.salt_seqs_destroy(self.ctx.h, self.h)
-        self.h = None
+        self._h = None
 
     def set_status(self, q_len, length, page_off, pages, domain=None, prefix_len=None, prefix_off=None,
                    prefix_pages=None, stream: int = 0) -> int:
