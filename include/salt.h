@@ -456,8 +456,8 @@ typedef struct {
 /* Validates the batch on the host (every length and page), cuts the attention's work and enqueues one
  * copy on `stream`.  Refused on a stream under capture, and for an object whose batch was recorded
  * into a graph (SALT_ERR_BAD_STATE): the recorded calls serve that batch for good, another one
- * takes another object and graph.  Errors: SALT_ERR_OUT_OF_RANGE (counts, lengths, pages, domains),
- * SALT_ERR_INVALID_ARG; the batch set before stays then. */
+ * takes another object and graph.  Errors: SALT_ERR_OUT_OF_RANGE (counts, lengths, pages, domains;
+ * launches of 2^32 threads), SALT_ERR_INVALID_ARG; the batch set before stays then. */
 SALT_API salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* seqs, const salt_seq_batch* batch, void* stream);
 
 /* Write the step's keys and values of one layer into the cache: row t of k and v is the step's
