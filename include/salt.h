@@ -476,7 +476,8 @@ SALT_API salt_status salt_kv_read(salt_ctx* ctx, salt_seqs* seqs, int32_t layer,
 /* Attention of the step's tokens over the cache, one layer: out[t][h] = sum_j p_j v_j with p =
  * softmax_j(scale q[t][h] . k_j), j over the whole prefix of the token's domain and its sequence's own
  * tokens up to its own place.  The step's keys and values are written first (salt_kv_write).  A prefix
- * that several short sequences share is read once for all of them.  A token without keys gives zeros.
+ * that several short sequences share is read once for all of them.  A token without keys gives zeros;
+ * a row with a logit of NaN or +inf, or with none above -inf, gives NaN.
  *   q [T][n_heads][head_dim], out the same: context dtype, rows ldq / ldo elements apart
  *   (0: dense; else a multiple of 8), 16-byte aligned; out may not overlap q.
  * The softmax's maximum and sum and the sum over v are fp32.  Reproducible bit for bit.

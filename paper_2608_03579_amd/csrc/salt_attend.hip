@@ -3,7 +3,8 @@
 //   out[t][h] = sum_j p_j v_j,   p = softmax_j(scale q[t][h] . k_j),
 //
 // j over the token's domain prefix (all of it) and its sequence's own keys up to the
-// token's own position; a row without keys gives zeros.  The batch is cut into work
+// token's own position; a row without keys gives zeros, a row whose logits are all -inf
+// NaN (as the formula does).  The batch is cut into work
 // items on the host (salt_seqs.h); a work item runs once per kv head.
 //
 // One pass over the keys with the running maximum m and sum l of the softmax.  Both
@@ -115,6 +116,14 @@ __device__ __forceinline__ float row_sum(float v) {
 // The running maximum follows a row's largest logit only when that is this much above it
 // (log2): exponentials stay below 2^8, and sums and products are seldom scaled anew.
 constexpr float kMaxSlack = 8.f;
+
+// What a row's weighted values are multiplied by in the end.  The largest logit above -inf has added about 1 or
+// more to the sum l, so l = 0 says that the row has no keys, or (0 / 0) none with a logit above -inf.
+__device__ __forceinline__ float inverse_sum(float l, bool has_keys) {
+  return l == 0.f ? (has_keys ? __builtin_nanf("") : 0.f) : 1.0f / l;
+}
+// Whether the rows of the tile's token `ti` have keys.  (asked where their keys are all in this item)
+__device__ __forceinline__ bool has_keys(const AttItem& it, int ti) { return it.pre_len > 0 || it.pos0 + ti >= 0; }
 
 // Word i of p, for a wave-uniform i: by way of the scalar unit.  (p is not written by this launch.)
 __device__ __forceinline__ int uniform_word(const int32_t* p, int i) {
@@ -267,7 +276,7 @@ __device__ __forceinline__ void finish_row(const AttArgs& a, const AttItem& it, 
     const int ti = row / a.group;
     E* out = reinterpret_cast<E*>(a.out) + (size_t)a.order[it.tok0 + ti] * a.ldo +
              (size_t)(kvh * a.group + row - ti * a.group) * D;
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    const float inv = inverse_sum(l, has_keys(it, ti));
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -384,7 +393,7 @@ __device__ __forceinline__ void attend_few(const AttArgs& a, const AttItem& it, 
     const int rt = row / a.group;
     E* out = reinterpret_cast<E*>(a.out) + (size_t)a.order[it.tok0 + rt] * a.ldo +
              (size_t)(kvh * a.group + row - rt * a.group) * D + d0;
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    const float inv = inverse_sum(l, has_keys(it, rt));
 #pragma unroll
     for (int d = 0; d < R::DT; d += 4) {
       if constexpr (sizeof(E) == 4)
@@ -785,7 +794,7 @@ __global__ void __launch_bounds__(256) k_attend_join(AttArgs a) {
     }
   }
   E* out = reinterpret_cast<E*>(a.out) + (size_t)j.tok * a.ldo + (size_t)h * D + d0;
-  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  const float inv = inverse_sum(l, true);                  // (salt_seqs.h: a joined row has keys)
 #pragma unroll
   for (int d = 0; d < DT; d += 4) {
     if constexpr (sizeof(E) == 4)

@@ -38,7 +38,8 @@ struct AttItem {
 };
 constexpr int kAllKeys = 1 << 30;
 // Pieces of one token, to be joined: `n` partial rows per query head, in two runs (its
-// own item's, and its domain's).  Partial row of piece p, kv head k and row r of the
+// own item's, and its domain's).  It has keys: a shared prefix is not empty, and a tile whose first tokens stand
+// before their sequence's first key, with no prefix, is too short to be cut.  Partial row of piece p, kv head k and row r of the
 // tile: row + (p * n_kv_heads + k) * stride + r.
 struct AttJoin {
   int32_t tok;
