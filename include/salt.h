@@ -356,8 +356,9 @@ SALT_API salt_status salt_adapter_gram(salt_ctx* ctx, const void* blob1, int32_t
  *     s = max(amax * (1/448), 2^-126),     code = e4m3(v * (1 / s)),
  *     y[t][o] <- rne( sum_kb s_x[t][kb] s_w[kb][o / 128] sum_{k in kb} xq[t][k] wq[k][o] ),
  *
- * accumulated in fp32.  A value that is not finite in x makes NaN of its token's y, one in W
- * of the outputs of its block.  A centroid is fused into W (salt_fuse_centroid) before W is pinned.
+ * accumulated in fp32.  A value that is not finite in x makes NaN of its token's y, one in W of its
+ * whole block, as it is held and in y at the block's outputs.  A centroid is fused into W
+ * (salt_fuse_centroid) before W is pinned.
  *
  * salt_pin_base: quantise table `table`'s W (device, context dtype, row-major [in][ldw], 16-byte
  * aligned, ldw a multiple of 8 and >= out_dim) into the context, which keeps the codes (1 byte

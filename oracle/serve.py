@@ -35,10 +35,11 @@ def _f32(a):
 
 
 def quantise_block(v: np.ndarray) -> np.ndarray:
-    """code * scale (float64) of one block."""
+    """code * scale (float64) of one block; NaN throughout where a value is not finite."""
     v = np.asarray(v, np.float64)
-    finite = np.abs(v[~np.isnan(v)])
-    amax = float(finite.max()) if finite.size else 0.0
+    if not np.isfinite(v).all():
+        return np.full(v.shape, np.nan)
+    amax = float(np.abs(v).max()) if v.size else 0.0
     with np.errstate(over="ignore", invalid="ignore"):
         s = np.maximum(_f32(np.float64(np.float32(amax)) * np.float64(np.float32(1.0 / 448.0))), np.float32(2.0 ** -126))
         r = _f32(1.0 / np.float64(s))

@@ -23,8 +23,8 @@ namespace {
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 constexpr float kE4m3Max = 448.f;
 
-// Scale of a block whose largest magnitude is amax (a NaN in the block does not
-// show in amax; it becomes a NaN code).
+// Scale of a block whose largest magnitude is amax, a number or infinity: with an infinite
+// scale every code times it is NaN.  (A NaN in x does not show in amax; its NaN code is enough for its token.)
 __device__ __forceinline__ float block_scale(float amax) { return fmaxf(amax * (1.0f / kE4m3Max), 0x1p-126f); }
 
 // Four codes of v * r, first in the lowest byte.
@@ -112,9 +112,10 @@ template <typename E>
 __global__ void __launch_bounds__(256) k_base_pin(BasePinArgs a) {
   __shared__ float s_v[kBaseBlock][kBaseBlock + 1];   // [input][output]
   __shared__ __attribute__((aligned(16))) uint8_t s_q[kBaseBlock * kPinLd];
-  __shared__ float s_max[4];
+  __shared__ uint32_t s_max[4];
   const int kb = blockIdx.x, nb = blockIdx.y, tid = threadIdx.x;
-  float amax = 0.f;
+  // the bits of the magnitudes order like the magnitudes, NaN above infinity
+  uint32_t amax = 0;
   for (int p = tid; p < kBaseBlock * (kBaseBlock / 8); p += 256) {
     const int k = p >> 4, o = (p & 15) * 8;
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -124,13 +125,14 @@ __global__ void __launch_bounds__(256) k_base_pin(BasePinArgs a) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       s_v[k][o + e] = v[e];
-      amax = fmaxf(amax, fabsf(v[e]));
+      amax = max(amax, __float_as_uint(v[e]) & 0x7fffffffu);
     }
   }
-  for (int m = 1; m < 64; m *= 2) amax = fmaxf(amax, __shfl_xor(amax, m));
+  for (int m = 1; m < 64; m *= 2) amax = max(amax, (uint32_t)__shfl_xor((int)amax, m));
   if ((tid & 63) == 0) s_max[tid >> 6] = amax;
   __syncthreads();
-  const float s = block_scale(fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3])));
+  const float top = __uint_as_float(max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3])));
+  const float s = top == top ? block_scale(top) : top;     // (a NaN takes the block, as an infinity does)
   const float r = 1.0f / s;
   for (int p = tid; p < kBaseBlock * (kBaseBlock / 4); p += 256) {
     const int o = p & 127, k = (p >> 7) * 4;
