@@ -364,13 +364,14 @@ SALT_API salt_status salt_adapter_gram(salt_ctx* ctx, const void* blob1, int32_t
  * aligned, ldw a multiple of 8 and >= out_dim) into the context, which keeps the codes (1 byte
  * a weight, out_dim padded to 256).  The first call also allocates the scratch that
  * products quantise x into (max_tokens x the widest in_dim bytes).  Enqueued on `stream`; W
- * may be freed once the stream has passed it.
+ * may be freed once the stream has passed it.  A table's first pin is refused on a stream under capture
+ * (SALT_ERR_BAD_STATE); a later one can be recorded.
  * salt_pin_base_fp8: the same from codes wq [out][ldq] (device, e4m3, row-major, 16-byte aligned,
  * ldq a multiple of 8 and >= in_dim) and any fp32 scales [ceil(out / 128)][ceil(in / 128)].
  * salt_read_base: the weight as it is held, code * scale, into w [in][ldw] in the context dtype.
  * Errors: SALT_ERR_OUT_OF_RANGE (table; more than 2^31 codes of a table or of the scratch),
  * SALT_ERR_INVALID_ARG (pointers, row length), SALT_ERR_OUT_OF_MEMORY, SALT_ERR_BAD_STATE
- * (salt_read_base of a table that was never pinned). */
+ * (salt_read_base of a table that was never pinned; under capture, as said). */
 SALT_API salt_status salt_pin_base(salt_ctx* ctx, int32_t table, const void* w, int64_t ldw, void* stream);
 SALT_API salt_status salt_pin_base_fp8(salt_ctx* ctx, int32_t table, const void* wq, int64_t ldq,
                                        const float* scales, void* stream);

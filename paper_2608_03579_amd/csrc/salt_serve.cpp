@@ -176,6 +176,14 @@ salt_status pin_args(salt_ctx* ctx, int32_t table, const void* w, int64_t ld, in
                     (long long)least);
   return SALT_OK;
 }
+// A table's first pin allocates, which a capture forbids, and makes its weight ready for calls that are not
+// recorded: it cannot be recorded itself.
+salt_status pin_capture(salt_ctx* ctx, int32_t table, hipStream_t s) {
+  const Base* b = static_cast<const Base*>(salt::ctx_base(ctx));
+  if (!(b && b->tab[(size_t)table].pinned) && is_capturing(s))
+    return ctx_fail(ctx, SALT_ERR_BAD_STATE, "the first pin of table %d on a stream under capture", table);
+  return SALT_OK;
+}
 
 }  // namespace
 
@@ -315,11 +323,11 @@ salt_status salt_pin_base(salt_ctx* ctx, int32_t table, const void* w, int64_t l
   SERVE_LIVE(ctx);
   const salt::CtxView v = salt::ctx_view(ctx);
   salt_status st = pin_args(ctx, table, w, ldw, table >= 0 && table < v.n_tables ? v.tables[table].out_dim : 0, v);
-  if (st != SALT_OK) return st;
-  Base* b = nullptr;
-  st = base_for(ctx, table, v, &b);
-  if (st != SALT_OK) return st;
   const hipStream_t s = (hipStream_t)stream;
+  if (st == SALT_OK) st = pin_capture(ctx, table, s);
+  Base* b = nullptr;
+  if (st == SALT_OK) st = base_for(ctx, table, v, &b);
+  if (st != SALT_OK) return st;
   if ((st = enter_stream(ctx, b->order, s)) != SALT_OK) return st;
   salt::BasePinArgs a{};
   a.w = const_cast<void*>(w);
@@ -340,10 +348,11 @@ salt_status salt_pin_base_fp8(salt_ctx* ctx, int32_t table, const void* wq, int6
   if (st != SALT_OK) return st;
   if (!scales || (reinterpret_cast<uintptr_t>(scales) & 3u))
     return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "null or misaligned scales");
-  Base* b = nullptr;
-  st = base_for(ctx, table, v, &b);
-  if (st != SALT_OK) return st;
   const hipStream_t s = (hipStream_t)stream;
+  st = pin_capture(ctx, table, s);
+  Base* b = nullptr;
+  if (st == SALT_OK) st = base_for(ctx, table, v, &b);
+  if (st != SALT_OK) return st;
   if ((st = enter_stream(ctx, b->order, s)) != SALT_OK) return st;
   salt::BasePinArgs a{};
   a.q = static_cast<const uint8_t*>(wq);
