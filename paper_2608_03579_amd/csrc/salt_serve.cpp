@@ -121,7 +121,12 @@ salt_status base_for(salt_ctx* ctx, int32_t table, const salt::CtxView& v, Base*
   if (!b) {
     b = new (std::nothrow) Base();
     if (!b) return ctx_fail(ctx, SALT_ERR_OUT_OF_MEMORY, "base weights");
-    b->tab.resize((size_t)v.n_tables);
+    try {
+      b->tab.resize((size_t)v.n_tables);
+    } catch (const std::bad_alloc&) {
+      free_base(b);
+      return ctx_fail(ctx, SALT_ERR_OUT_OF_MEMORY, "base weights");
+    }
     int in = 0;
     for (int t = 0; t < v.n_tables; ++t) in = std::max(in, v.tables[t].in_dim);
     b->kb_max = ceil_div(in, salt::kBaseBlock);

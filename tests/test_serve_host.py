@@ -24,7 +24,7 @@ def serve_host(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("check", ["capture"])
+@pytest.mark.parametrize("check", ["capture", "memory"])
 def test_serve_host(serve_host, check):
     res = subprocess.run([serve_host, check], capture_output=True, text=True, timeout=120)
     assert res.returncode == 0 and res.stdout.strip().endswith("ok"), res.stdout + res.stderr
