@@ -13,6 +13,7 @@
 
 #include <algorithm>
 
+#include "salt_base_rule.h"
 #include "salt_device.h"
 #include "salt_layout.h"
 #include "salt_serve.h"
@@ -582,42 +583,23 @@ hipError_t launch_tile(BaseArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Which kernel: the largest tile whose blocks still fill the device, since a larger one reads
-// less per product.  us of one product (quantised x included), by tile:
-//   outputs x inputs, tokens    256 x 256   128 x 256   128 x 128   64 x 64   32 x 64   32 x 32
-//   16384 x 3072, 1024               57          64          76       136       130       214
-//   16384 x 3072,  512               48          36          41        73        69       110
-//    4096 x 4096, 2048               64          49          54        71        82        95
-//    4096 x 4096,  256               54          35          32        14        16        18
-//    4096 x 4096,  128               51          33          31        12        11        12
-//    4096 x 4096,   64               50          32          30        12        11        10
-// The first three walk all inputs in each block, the others split them over a block's waves.
 template <typename E>
 hipError_t product(BaseArgs& a, int n_cu, hipStream_t s) {
-  auto blocks = [&](int outs, int toks) {
-    int64_t n = 0;
-    for (int i = 0; i < a.n_tables; ++i) n += cdiv(a.tab[i].out, outs);
-    return n * cdiv(a.T, toks);
-  };
-  // Few tokens: no launch ahead of the product's.  28672 x 4096 of one token 25 us in this way and
-  // 36 behind the quantiser, 3072 x 3072 4.6 and 7.5, of 16 tokens 5.8 and 7.7; in fp32, with
-  // twice the x to read in every block, 8 tokens 6.5 and 7.3, 16 tokens 8.7 and 7.6.  Two
-  // output tiles to a block where one each would not run at once (6144 x 4096: 6.0 and 8.3 us).
-  if (a.T <= (sizeof(E) == 2 ? 16 : 8)) {
-    if (blocks(16, 16) <= n_cu)
+  const BaseKernel kernel = base_kernel([&](int i) { return a.tab[i].out; }, a.n_tables, a.T, sizeof(E), n_cu);
+  if (kernel == kBaseFew1 || kernel == kBaseFew2) {
+    if (kernel == kBaseFew1)
       hipLaunchKernelGGL((k_base_few<E, 1>), dim3(number_items(a, 32, 2)), dim3(64 * kFewWaves), 0, s, a);
     else hipLaunchKernelGGL((k_base_few<E, 2>), dim3(number_items(a, 32)), dim3(64 * kFewWaves), 0, s, a);
     return hipGetLastError();
   }
   hipLaunchKernelGGL(k_base_quantise<E>, dim3(cdiv(a.T, 16), cdiv(a.kb, 4)), dim3(256), 0, s, a);
-  const int64_t most = (int64_t)n_cu * 7 / 10, some = (int64_t)n_cu * 6 / 10;
-  if constexpr (sizeof(E) == 2) {       // (bf16 operands of fp32 contexts take twice the registers)
-    if (blocks(256, 256) >= most) return launch_tile<E, 8, 4, 2, 4>(a, s);
-    if (blocks(128, 256) >= most) return launch_tile<E, 4, 4, 2, 4>(a, s);
+  if constexpr (sizeof(E) == 2) {
+    if (kernel == kBaseTile256x256) return launch_tile<E, 8, 4, 2, 4>(a, s);
+    if (kernel == kBaseTile128x256) return launch_tile<E, 4, 4, 2, 4>(a, s);
   }
-  if (blocks(128, 128) >= most) return launch_tile<E, 4, 4, 2, 2>(a, s);
-  if (blocks(64, 64) >= some) return launch_split<E, 4, 4>(a, s);
-  if (blocks(32, 64) >= some) return launch_split<E, 2, 4>(a, s);
+  if (kernel == kBaseTile128x128) return launch_tile<E, 4, 4, 2, 2>(a, s);
+  if (kernel == kBaseSplit64x64) return launch_split<E, 4, 4>(a, s);
+  if (kernel == kBaseSplit32x64) return launch_split<E, 2, 4>(a, s);
   return launch_split<E, 2, 2>(a, s);
 }
 
