@@ -8,6 +8,9 @@ Users of two domains share their domain's prompt. Per step:
     attention over prompt and history    salt_attend         (a domain's prompt is read once)
     y = attention W_o, += the adapters   salt_base_product, salt_apply
 
+This block encodes no positions. A model that rotates q and k does so with a kernel of its own between the second
+line and the third: libsalt has no such operator.
+
     python examples/attention_block.py [steps]
 
 Runs on synthetic values (seeded) and compares the last step's output with float64 arithmetic on

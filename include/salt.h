@@ -356,9 +356,12 @@ SALT_API salt_status salt_adapter_gram(salt_ctx* ctx, const void* blob1, int32_t
  *     s = max(amax * (1/448), 2^-126),     code = e4m3(v * (1 / s)),
  *     y[t][o] <- rne( sum_kb s_x[t][kb] s_w[kb][o / 128] sum_{k in kb} xq[t][k] wq[k][o] ),
  *
- * accumulated in fp32.  A value that is not finite in x makes NaN of its token's y, one in W of its
- * whole block, as it is held and in y at the block's outputs.  A centroid is fused into W
- * (salt_fuse_centroid) before W is pinned.
+ * the sum over the blocks in fp32.  The 128 products of a block are summed in fp32 in fp32
+ * contexts; in bf16 contexts by one 8-bit matrix instruction, which keeps some 14 bits behind the
+ * largest of them (1.4e-5 of y's size where x and W are random, a hundredth of y's own rounding).
+ * A value that is not finite in x makes NaN of its token's y, one in W of its whole block, as it
+ * is held and in y at the block's outputs.  A centroid is fused into W (salt_fuse_centroid)
+ * before W is pinned.
  *
  * salt_pin_base: quantise table `table`'s W (device, context dtype, row-major [in][ldw], 16-byte
  * aligned, ldw a multiple of 8 and >= out_dim) into the context, which keeps the codes (1 byte
@@ -383,7 +386,9 @@ SALT_API salt_status salt_read_base(salt_ctx* ctx, int32_t table, void* w, int64
  * 0 <= T <= max_tokens.  Enqueued on `stream`; nothing is allocated, and results are
  * reproducible bit for bit.  The products of a context share its scratch: the library orders them,
  * also across streams, so the stream of the latest one must stay valid until the next, or until
- * salt_destroy; recorded into a graph, all go to the one stream.  Errors: SALT_ERR_OUT_OF_RANGE
+ * salt_destroy; recorded into a graph, all go to the one stream.  A graph's launch is not a call
+ * that the library sees: a program that launches recorded products orders them itself against
+ * products on other streams (on one stream they are in order).  Errors: SALT_ERR_OUT_OF_RANGE
  * (table, T), SALT_ERR_BAD_STATE (a base weight never pinned; under capture behind work on
  * another stream), SALT_ERR_INVALID_ARG; nothing is enqueued then. */
 SALT_API salt_status salt_base_product(salt_ctx* ctx, int32_t n, const int32_t* tables, int32_t T, const void* x,
@@ -428,8 +433,9 @@ SALT_API void salt_kv_destroy(salt_ctx* ctx, salt_kv* kv);
  * salt_seqs_destroy (which waits for the device), with its cache, or with the context.  Its work,
  * and that of a cache, is ordered by the library across streams (the stream of the latest call must
  * stay valid until the next one, or the object's end; work under capture stays on one stream, else
- * SALT_ERR_BAD_STATE); streams that are to run concurrently need objects of their own, and a cache
- * each. */
+ * SALT_ERR_BAD_STATE).  A graph's launch is not a call that the library sees: a program that
+ * launches recorded work of an object or a cache orders it itself against calls on other streams.
+ * Streams that are to run concurrently need objects of their own, and a cache each. */
 SALT_API salt_status salt_seqs_create(salt_ctx* ctx, salt_kv* kv, int32_t max_seqs, int32_t max_tokens,
                                       int32_t max_pages, salt_seqs** out);
 SALT_API void salt_seqs_destroy(salt_ctx* ctx, salt_seqs* seqs);
@@ -477,12 +483,21 @@ SALT_API salt_status salt_kv_read(salt_ctx* ctx, salt_seqs* seqs, int32_t layer,
 
 /* Attention of the step's tokens over the cache, one layer: out[t][h] = sum_j p_j v_j with p =
  * softmax_j(scale q[t][h] . k_j), j over the whole prefix of the token's domain and its sequence's own
- * tokens up to its own place.  The step's keys and values are written first (salt_kv_write).  A prefix
+ * tokens up to its own place.  Positions enter nowhere: where a model rotates q and k, the caller
+ * does, between the apply and salt_kv_write / salt_attend.  The step's keys and values are written first (salt_kv_write).  A prefix
  * that several short sequences share is read once for all of them.  A token without keys gives zeros;
  * a row with a logit of NaN or +inf, or with none above -inf, gives NaN.
  *   q [T][n_heads][head_dim], out the same: context dtype, rows ldq / ldo elements apart
  *   (0: dense; else a multiple of 8), 16-byte aligned; out may not overlap q.
- * The softmax's maximum and sum and the sum over v are fp32.  Reproducible bit for bit.
+ * The softmax's maximum and sum and the sum over v are fp32.  Reproducible bit for bit.  q and the
+ * cache's values enter the products unrounded (fp32 q with 24 bits), the probabilities with 24 bits
+ * in fp32 contexts and 16 in bf16 contexts, but for one case: in bf16 contexts over SALT_KV_E4M3,
+ * where more than 16 rows (tokens times the query heads of a kv head) read the same keys, they
+ * enter with 8 bits over runs of 64 keys that all of a tile of those rows see, p then divided by
+ * the sum of the rounded ones.  An error of up to 2^-9 of sum_j p_j |v_j| and of out, beside out's
+ * own rounding (2^-9); which tokens it meets depends on the batch.
+ * For finite results |q| <= 2^110, |v| <= 2^119 / keys and logits within fp32 suffice (weights may
+ * stand at 2^8 before the division); beyond, a row may be infinite or NaN where the formula is not.
  * Errors of these three calls: SALT_ERR_BAD_STATE (no batch set), SALT_ERR_OUT_OF_RANGE (layer),
  * SALT_ERR_INVALID_ARG (pointers, row lengths, scale not finite or <= 0). */
 SALT_API salt_status salt_attend(salt_ctx* ctx, salt_seqs* seqs, int32_t layer, const void* q, int64_t ldq,

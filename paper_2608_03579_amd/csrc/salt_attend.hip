@@ -11,8 +11,10 @@
 // products run on bf16 matrix instructions with fp32 accumulation: every code of the
 // cache is exact in bf16 and its scale multiplies the fp32 logit (k) or probability
 // (v), so nothing of the cache is rounded again.  In bf16 contexts q enters as it is and the
-// probabilities in two bf16 terms (16 bits: one term's 2^-8 would show beside the
+// probabilities in two bf16 terms (16 bits: one term's 2^-9 would show beside the
 // result's own rounding where a row has few keys); in fp32 contexts both enter in three, 24 bits.
+// One term is taken in one place: tiles of more than 16 rows over e4m3, for units that all rows see
+// whole (attend_many, which says why): an error of up to 2^-9 of sum p|v| and of out there.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
