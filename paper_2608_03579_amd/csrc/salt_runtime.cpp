@@ -197,7 +197,7 @@ struct salt_ctx {
   std::vector<std::pair<void*, salt::OwnedFree>> owned;
   void* base = nullptr;                  // the base weights among them
   bool poisoned = false;
-  std::string err;
+  char err[512] = "";                    // the last failure's message (kept where host memory is out, too)
 };
 
 namespace {
@@ -207,12 +207,12 @@ thread_local std::string g_create_err;
 
 salt_status fail(salt_ctx* c, salt_status s, const char* fmt, ...) {
   if (c) {
-    char buf[512];
+    char buf[sizeof c->err];               // (an argument may be the message before)
     va_list ap;
     va_start(ap, fmt);
     vsnprintf(buf, sizeof buf, fmt, ap);
     va_end(ap);
-    c->err = buf;
+    snprintf(c->err, sizeof c->err, "%s", buf);
   }
   return s;
 }
@@ -220,7 +220,7 @@ salt_status fail(salt_ctx* c, salt_status s, const char* fmt, ...) {
 salt_status hip_fail(salt_ctx* c, hipError_t e, const char* what) {
   if (c) {
     c->poisoned = true;
-    c->err = std::string(what) + ": " + hipGetErrorString(e);
+    snprintf(c->err, sizeof c->err, "%s: %s", what, hipGetErrorString(e));
   }
   return SALT_ERR_HIP;
 }
@@ -234,7 +234,7 @@ salt_status hip_fail(salt_ctx* c, hipError_t e, const char* what) {
 #define SALT_LIVE(ctx)                                                                          \
   do {                                                                                          \
     if (!(ctx)) return SALT_ERR_INVALID_ARG;                                                    \
-    if ((ctx)->poisoned) return fail((ctx), SALT_ERR_BAD_STATE, "context is poisoned: %s", (ctx)->err.c_str()); \
+    if ((ctx)->poisoned) return fail((ctx), SALT_ERR_BAD_STATE, "context is poisoned: %s", (ctx)->err); \
   } while (0)
 
 // dst[i][o][j] = src[i][j][o] for n matrices of rc x out elements.
@@ -855,7 +855,7 @@ const char* salt_status_str(salt_status s) {
   return "unknown status";
 }
 
-const char* salt_last_error(const salt_ctx* ctx) { return ctx ? ctx->err.c_str() : g_create_err.c_str(); }
+const char* salt_last_error(const salt_ctx* ctx) { return ctx ? ctx->err : g_create_err.c_str(); }
 
 int32_t salt_version(void) { return SALT_VERSION; }
 
@@ -940,7 +940,7 @@ salt_status salt_create(const salt_config* cfg, salt_ctx** out) {
 
   auto bail = [&](salt_status st, hipError_t e, const char* what) {
     if (st == SALT_ERR_HIP) hip_fail(c, e, what);
-    else c->err = "device allocation failed";
+    else fail(c, st, "device allocation failed");
     g_create_err = c->err;
     destroy_ctx_memory(c);
     delete c;
