@@ -483,8 +483,8 @@ SALT_API salt_status salt_kv_read(salt_ctx* ctx, salt_seqs* seqs, int32_t layer,
 
 /* Attention of the step's tokens over the cache, one layer: out[t][h] = sum_j p_j v_j with p =
  * softmax_j(scale q[t][h] . k_j), j over the whole prefix of the token's domain and its sequence's own
- * tokens up to its own place.  Positions enter nowhere: where a model rotates q and k, the caller
- * does, between the apply and salt_kv_write / salt_attend.  The step's keys and values are written first (salt_kv_write).  A prefix
+ * tokens up to its own place.  Positions enter nowhere: a model that rotates q and k does so between
+ * the apply and salt_kv_write / salt_attend (salt_rotate).  The step's keys and values are written first (salt_kv_write).  A prefix
  * that several short sequences share is read once for all of them.  A token without keys gives zeros;
  * a row with a logit of NaN or +inf, or with none above -inf, gives NaN.
  *   q [T][n_heads][head_dim], out the same: context dtype, rows ldq / ldo elements apart
@@ -502,6 +502,108 @@ SALT_API salt_status salt_kv_read(salt_ctx* ctx, salt_seqs* seqs, int32_t layer,
  * SALT_ERR_INVALID_ARG (pointers, row lengths, scale not finite or <= 0). */
 SALT_API salt_status salt_attend(salt_ctx* ctx, salt_seqs* seqs, int32_t layer, const void* q, int64_t ldq,
                                  void* out, int64_t ldo, float scale, void* stream);
+
+/* ---- norms and rotation of q and k ------------------------------------------------------------
+ * Between the apply and the cache: every head x (head_dim = D values) of q and of k, each with its own
+ * norm, in one pass.
+ *
+ *     v = x / sqrt(mean(x^2) + eps) * norm           (norm NULL: v = x)
+ *     (a, b) <- gain * (a cos t - b sin t, b cos t + a sin t),   t = pos * freq[i],
+ *
+ * for the pairs (a, b) of v's first R = rot_dim values: (v[i], v[i + R/2]), or with interleaved = 1
+ * (v[2i], v[2i + 1]), i < R/2; the values behind them stay as they are.  fp32 throughout, rounded once at
+ * the end; the angle is reduced in 64 bits, so far positions keep their place on the circle (an error of
+ * 2^-21 of the pair's length up to |t| = 2^31).  |x| <= 2^60 with a norm (its square is summed in fp32). */
+typedef struct {
+  int32_t n_heads, n_kv_heads;  /* of q and of k, at most 65536 each; 0: that operand is not touched   */
+  int32_t head_dim;             /* a multiple of 8 in [8, 256]                                        */
+  int32_t rot_dim;              /* a multiple of 8 in [8, head_dim]                                   */
+  int32_t interleaved;          /* 0: pairs half the rotated values apart; 1: side by side            */
+  const double* freq;           /* host, [rot_dim / 2], radians per position, |freq| <= 10^4; read by the call */
+  const void* q_norm;           /* device, [head_dim] context dtype, 16-byte aligned, or NULL           */
+  const void* k_norm;
+  float eps;                    /* >= 0                                                               */
+  float gain;                   /* of the rotated pairs; 1 for a plain rotation                       */
+} salt_rotation;
+/* T tokens at pos[T] (device, any int32): q [T][n_heads][head_dim] into q_out, k [T][n_kv_heads][head_dim]
+ * into k_out: context dtype, rows ld elements apart (0: dense; else a multiple of 8), 16-byte aligned.  In
+ * place (q_out == q with equal rows), or without overlap.  0 <= T <= 2^20 whatever max_tokens.  No
+ * scratch: calls on different streams do not meet.  Errors: SALT_ERR_INVALID_ARG, SALT_ERR_OUT_OF_RANGE (T). */
+SALT_API salt_status salt_rotate(salt_ctx* ctx, const salt_rotation* rot, int32_t T, const int32_t* pos, const void* q,
+                                 int64_t ldq, void* q_out, int64_t ldqo, const void* k, int64_t ldk, void* k_out,
+                                 int64_t ldko, void* stream);
+
+/* ---- a bounded cache: gathered weights and eviction ----------------------------------------------
+ * A tracked cache keeps two marks with every token, layer and kv head: the attention weight that the
+ * token has gathered from the queries so far (fp32), and its position.  A server that holds its
+ * sequences to a budget scores each step and evicts the tokens of least weight:
+ *     salt_kv_write, salt_attend, salt_kv_score, [salt_kv_evict]   for every layer of a step.
+ *
+ * salt_kv_track allocates the marks of every layer and page and clears them (blocking, once; a
+ * second call does nothing).  Errors: SALT_ERR_INVALID_ARG, SALT_ERR_OUT_OF_MEMORY. */
+SALT_API salt_status salt_kv_track(salt_ctx* ctx, salt_kv* kv);
+/* After salt_kv_write of the step, with the q and scale of salt_attend: to token j of a sequence, for each
+ * kv head, add
+ *     w_j = sum_t sum_h softmax_i(scale q[t][h] . k_i)[j]
+ * over the sequence's counted new tokens t that see j and the query heads h of the kv head; i runs over all
+ * keys of salt_attend, a domain's prefix too.  Counted are the last `window` new tokens of each sequence,
+ * all of them for window = 0.  The step's own new tokens start at w_j, whatever their marks
+ * held, and take the position pos[t] (device, [T]; NULL: their place in the sequence); so each step
+ * is scored once.  A prefix has no marks.  A row with a logit of NaN or +inf, or none above -inf, adds NaN
+ * to all that it sees.  fp32 sums, reproducible bit for bit; q and keys as in salt_attend, the weights unrounded. */
+SALT_API salt_status salt_kv_score(salt_ctx* ctx, salt_seqs* seqs, int32_t layer, const void* q, int64_t ldq,
+                                   const int32_t* pos, float scale, int32_t window, void* stream);
+/* For every sequence of the batch with n = len > keep own tokens, each kv head by itself, keep `keep` tokens:
+ * first those whose position is among the newest (position > newest - recent), then those of
+ * the largest gathered weight (NaN above all numbers); equals by the lower place.  The kept tokens behind
+ * place `keep` move, with their marks, to the places of the dropped ones before it, in order; the places
+ * from `keep` on are left as they were.  The sequence then has `keep` tokens in its first
+ * pages: the next batch says so (len = keep + its new tokens).  Order within a sequence means nothing to
+ * salt_attend, whose q and k carry their positions; kv heads no longer hold the same tokens at a place.
+ * 0 <= recent <= keep; sequences of at most 2^19 tokens (SALT_ERR_OUT_OF_RANGE). */
+SALT_API salt_status salt_kv_evict(salt_ctx* ctx, salt_seqs* seqs, int32_t layer, int32_t keep, int32_t recent,
+                                   void* stream);
+/* The marks of all own tokens of sequence 0, then 1, and so on, out of the cache or into it (a sequence that
+ * moves from one node to another): weight and pos are device arrays [sum of len][n_kv_heads], 16-byte aligned.
+ * Errors of these four calls: as salt_attend, and SALT_ERR_BAD_STATE for a cache that is not tracked; those that
+ * change marks refuse a batch in which a page holds own tokens of two sequences, or of a sequence and
+ * a domain (SALT_ERR_INVALID_ARG). */
+SALT_API salt_status salt_kv_read_marks(salt_ctx* ctx, salt_seqs* seqs, int32_t layer, float* weight, int32_t* pos,
+                                        void* stream);
+SALT_API salt_status salt_kv_write_marks(salt_ctx* ctx, salt_seqs* seqs, int32_t layer, const float* weight,
+                                         const int32_t* pos, void* stream);
+
+/* ---- beam search over the cache's sequences ------------------------------------------------------
+ * A request's beams are sequences that share pages of their past; each step keeps the best continuations
+ * of all of them:
+ *     salt_beam_select, [the host reads the beams], salt_kv_copy of the last pages of beams that go on
+ *     more than once, salt_seqs_set with the new page tables.
+ * (A full page may stand in the tables of several sequences; the one that new tokens go into may not.)
+ *
+ * salt_beams is an object that owns scratch for up to max_rows beams (at most 65536) of a call and max_out (at most
+ * 64) continuations of a request; its work is ordered by the library across streams, as that of salt_seqs. */
+typedef struct salt_beams salt_beams;
+SALT_API salt_status salt_beams_create(salt_ctx* ctx, int32_t max_rows, int32_t max_out, salt_beams** out);
+SALT_API void salt_beams_destroy(salt_ctx* ctx, salt_beams* beams);
+/* n_reqs requests of `width` beams each (1 to 64), logits [n_reqs * width][ld] (device, context dtype, 16-byte
+ * aligned; ld 0: dense, else a multiple of 8; vocab in [1, 2^24]), score [n_reqs * width] (device, fp32) the beams' own log
+ * probabilities.  Of a request's continuations (beam b, token v), worth
+ *     score[b] + logits[b][v] - log sum_u exp logits[b][u],
+ * the n_out best in order, ties by the lower beam, then the lower token: their worth, beam (0 to width - 1)
+ * and token, each [n_reqs][n_out] (device).  A beam with a score that is not finite (-inf: one that is not live), with a
+ * logit of NaN or +inf, or with none above -inf offers nothing, and no beam offers a token of logit -inf; where
+ * there are too few, the rest are (-inf, -1, -1).  The order within a beam is exactly that of the logits; exponentials are
+ * fp32, their sum and the worth 64 bits (the worth rounded to fp32 on output).
+ * Errors: SALT_ERR_OUT_OF_RANGE (counts), SALT_ERR_INVALID_ARG (pointers, rows), SALT_ERR_BAD_STATE (capture, as
+ * salt_base_product). */
+SALT_API salt_status salt_beam_select(salt_ctx* ctx, salt_beams* beams, int32_t n_reqs, int32_t width, int32_t vocab,
+                                      const void* logits, int64_t ld, const float* score, int32_t n_out,
+                                      float* out_score, int32_t* out_beam, int32_t* out_token, void* stream);
+/* In every layer, page dst[i] becomes a copy of page src[i] (keys, values, marks), or of its first tokens[i] tokens
+ * (NULL: all), for i < n; host arrays, read before the call returns.  No page is written twice or
+ * both read and written (SALT_ERR_INVALID_ARG).  Ordered with the cache's other work. */
+SALT_API salt_status salt_kv_copy(salt_ctx* ctx, salt_kv* kv, int32_t n, const int32_t* src, const int32_t* dst,
+                                  const int32_t* tokens, void* stream);
 
 /* ---- centroid routing (host only) ------------------------------------------------------
  * Sec. 3.2: a user's dataset is routed to a centroid of the library, or to the

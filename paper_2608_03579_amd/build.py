@@ -15,8 +15,9 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsalt.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("salt_plan.hip", "salt_apply.hip", "salt_fuse_gram.hip", "salt_swap.hip",
-                                           "salt_base.hip", "salt_kv.hip", "salt_attend.hip", "salt_runtime.cpp",
-                                           "salt_serve.cpp")]
+                                           "salt_base.hip", "salt_kv.hip", "salt_attend.hip", "salt_rotate.hip",
+                                           "salt_marks.hip", "salt_beam.hip", "salt_runtime.cpp", "salt_serve.cpp",
+                                           "salt_decode.cpp")]
 ARCH = "gfx950"
 
 BUILD_DIR = os.path.join(HERE, "_build")

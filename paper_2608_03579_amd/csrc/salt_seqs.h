@@ -47,6 +47,11 @@ struct AttJoin {
   int32_t pad_;
 };
 
+// A sequence of the batch: its first row of q, its new and its own tokens, its first page reference.
+struct SeqRec {
+  int32_t tok0, q_len, len, ref0;
+};
+
 struct SeqBatch {
   int n_seqs, n_domains;
   const int32_t* q_len;

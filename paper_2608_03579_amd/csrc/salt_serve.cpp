@@ -13,67 +13,25 @@
 #include <vector>
 
 #include "salt.h"
+#include "salt_objects.h"
 #include "salt_seqs.h"
 #include "salt_serve.h"
 
 namespace {
 
+using salt::aligned16;
+using salt::batch_call;
+using salt::ceil_div;
 using salt::ctx_fail;
-
-#define SERVE_LIVE(ctx)                                  \
-  do {                                                   \
-    const salt_status st_ = salt::ctx_live(ctx);         \
-    if (st_ != SALT_OK) return st_;                      \
-  } while (0)
-#define SERVE_HIP(ctx, call)                                              \
-  do {                                                                    \
-    hipError_t e_ = (call);                                               \
-    if (e_ != hipSuccess) return salt::ctx_hip_fail((ctx), e_, #call);    \
-  } while (0)
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
-int ceil_div(int a, int b) { return (a + b - 1) / b; }
-
-bool is_capturing(hipStream_t s) {
-  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(s, &cap) != hipSuccess) {
-    (void)hipGetLastError();
-    return false;
-  }
-  return cap == hipStreamCaptureStatusActive;
-}
-
-// Work on an object's buffers goes to `s`: behind what went to another stream before.
-struct StreamOrder {
-  hipEvent_t hop = nullptr;
-  hipStream_t last = nullptr;
-  bool used = false;
-  hipError_t enter(hipStream_t s) {
-    if (used && last != s) {
-      hipError_t e = hipSuccess;
-      if (!hop) e = hipEventCreateWithFlags(&hop, hipEventDisableTiming);
-      if (e == hipSuccess) e = hipEventRecord(hop, last);
-      if (e == hipSuccess) e = hipStreamWaitEvent(s, hop, 0);
-      if (e != hipSuccess) return e;
-    }
-    used = true;
-    last = s;
-    return hipSuccess;
-  }
-  // Work under capture cannot be ordered against work outside it.
-  bool refuses(hipStream_t s) const { return used && last != s && (is_capturing(s) || is_capturing(last)); }
-  void destroy() {
-    if (hop) (void)hipEventDestroy(hop);
-    hop = nullptr;
-  }
-};
-salt_status enter_stream(salt_ctx* ctx, StreamOrder& o, hipStream_t s) {
-  if (o.refuses(s))
-    return ctx_fail(ctx, SALT_ERR_BAD_STATE, "work under capture on another stream than the object's last work");
-  SERVE_HIP(ctx, o.enter(s));
-  return SALT_OK;
-}
+using salt::enter;
+using salt::enter_stream;
+using salt::is_capturing;
+using salt::kv_of;
+using salt::layer_of;
+using salt::round_up;
+using salt::rows_arg;
+using salt::seqs_of;
+using salt::StreamOrder;
 
 // The base weights of a context: per table codes and scales, and the scratch that the
 // products quantise x into.
@@ -192,40 +150,6 @@ salt_status pin_capture(salt_ctx* ctx, int32_t table, hipStream_t s) {
 
 }  // namespace
 
-// ---- KV cache objects --------------------------------------------------------------------
-struct salt_kv {
-  salt_kv_config cfg{};
-  int log2_page = 0;
-  char* pool = nullptr;
-  size_t codes = 0, scales = 0;       // bytes of one layer's k (or v) codes, and scales
-  std::vector<salt_seqs*> seqs;
-  std::vector<uint32_t> stamp;        // per page: the salt_seqs_set that last saw it written
-  uint32_t stamps = 0;
-  StreamOrder order;                  // writes and reads of the pool
-};
-
-struct salt_seqs {
-  salt_kv* kv = nullptr;
-  int max_seqs = 0, max_tokens = 0, max_pages = 0;
-  size_t words = 0;                   // 32-bit words of one staging buffer
-  int32_t* dev = nullptr;
-  int32_t* staging = nullptr;         // two page-locked buffers
-  int stage = 0;
-  hipEvent_t staged[2] = {};
-  bool pending[2] = {};
-  float *part = nullptr, *stat = nullptr;
-  int64_t part_rows = 0;
-  StreamOrder order;
-  // the batch
-  int T = -1;                         // -1: none was set
-  int n_refs = 0, n_own_refs = 0;
-  int64_t own_tokens = 0;
-  bool clash = false;                 // two of its tokens' pages are one page
-  bool recorded = false;              // a graph holds its launches: grid sizes and places in `dev`
-  size_t at_page = 0, at_row = 0, at_count = 0, at_slot = 0, at_order = 0, at_item = 0, at_join = 0;
-  int n_kind[4] = {0, 0, 0, 0}, n_joins = 0;
-};
-
 namespace {
 
 void free_seqs(salt_seqs* q) {
@@ -242,6 +166,7 @@ void free_kv(void* p) {
   salt_kv* kv = static_cast<salt_kv*>(p);
   for (salt_seqs* q : kv->seqs) free_seqs(q);
   if (kv->pool) (void)hipFree(kv->pool);
+  if (kv->marks) (void)hipFree(kv->marks);
   kv->order.destroy();
   delete kv;
 }
@@ -264,59 +189,6 @@ void kv_sizes(const salt_kv_config& c, size_t* codes, size_t* scales) {
   const size_t vecs = (size_t)c.n_pages * c.n_kv_heads * c.page_tokens;
   *codes = round_up(vecs * (size_t)c.head_dim, 256);
   *scales = round_up(vecs * sizeof(float), 256);
-}
-
-// Whether `kv` is a live cache of `ctx` (asked before anything of it is read).
-salt_status kv_of(salt_ctx* ctx, const salt_kv* kv) {
-  if (!kv || !salt::ctx_owns(ctx, kv)) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "not a cache of this context");
-  return SALT_OK;
-}
-salt_status seqs_of(salt_ctx* ctx, const salt_seqs* q) {
-  if (!q) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "null sequences");
-  return kv_of(ctx, q->kv);
-}
-
-salt::KvLayer layer_of(const salt_kv* kv, int layer) {
-  salt::KvLayer l{};
-  char* p = kv->pool + (size_t)layer * 2 * (kv->codes + kv->scales);
-  l.k = reinterpret_cast<uint8_t*>(p);
-  l.v = reinterpret_cast<uint8_t*>(p + kv->codes);
-  l.ks = reinterpret_cast<float*>(p + 2 * kv->codes);
-  l.vs = reinterpret_cast<float*>(p + 2 * kv->codes + kv->scales);
-  l.kv_heads = kv->cfg.n_kv_heads;
-  l.dim = kv->cfg.head_dim;
-  l.log2_page = kv->log2_page;
-  l.format = kv->cfg.format;
-  return l;
-}
-
-// Common checks of the calls on a set batch.
-salt_status batch_call(salt_ctx* ctx, salt_seqs* q, int32_t layer) {
-  SERVE_LIVE(ctx);
-  const salt_status st = seqs_of(ctx, q);
-  if (st != SALT_OK) return st;
-  if (q->T < 0) return ctx_fail(ctx, SALT_ERR_BAD_STATE, "no batch was set on the sequences");
-  if (layer < 0 || layer >= q->kv->cfg.n_layers)
-    return ctx_fail(ctx, SALT_ERR_OUT_OF_RANGE, "layer %d not in [0, %d)", layer, q->kv->cfg.n_layers);
-  return SALT_OK;
-}
-// A row-major operand of whole heads: rows `ld` elements apart (0: dense).
-salt_status rows_arg(salt_ctx* ctx, const char* what, const void* p, int64_t& ld, int64_t width) {
-  if (ld == 0) ld = width;
-  if (!p || !aligned16(p)) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "null or misaligned %s", what);
-  if (ld < width || ld % 8 != 0)
-    return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "%s rows of %lld elements: need a multiple of 8 and >= %lld", what,
-                    (long long)ld, (long long)width);
-  return SALT_OK;
-}
-// The batch's buffers and the pool, on `s`.
-salt_status enter(salt_ctx* ctx, salt_seqs* q, hipStream_t s) {
-  if (q->kv->order.refuses(s))
-    return ctx_fail(ctx, SALT_ERR_BAD_STATE, "work under capture on another stream than the cache's last work");
-  salt_status st = enter_stream(ctx, q->order, s);
-  if (st == SALT_OK) st = enter_stream(ctx, q->kv->order, s);
-  if (st == SALT_OK && is_capturing(s)) q->recorded = true;
-  return st;
 }
 
 }  // namespace
@@ -461,6 +333,7 @@ salt_status salt_kv_create(salt_ctx* ctx, const salt_kv_config* cfg, salt_kv** o
   const size_t bytes = salt_kv_bytes(cfg);
   try {
     kv->stamp.assign((size_t)cfg->n_pages, 0);
+    kv->held.assign((size_t)cfg->n_pages, 0);
   } catch (const std::bad_alloc&) {
     free_kv(kv);
     return ctx_fail(ctx, SALT_ERR_OUT_OF_MEMORY, "cache");
@@ -514,8 +387,8 @@ salt_status salt_seqs_create(salt_ctx* ctx, salt_kv* kv, int32_t max_seqs, int32
   q->max_pages = max_pages;
   const size_t T = (size_t)max_tokens;
   const size_t items = (size_t)salt::attend_max_items(max_tokens, kv->cfg.n_heads);
-  // (each of the six arrays behind the first starts at a multiple of 16 words)
-  q->words = 3 * (size_t)max_pages + 3 * T + 6 * 16 + items * (sizeof(salt::AttItem) / 4) + T * (sizeof(salt::AttJoin) / 4);
+  // (each of the nine arrays behind the first starts at a multiple of 16 words)
+  q->words = 4 * (size_t)max_pages + 4 * T + (sizeof(salt::SeqRec) / 4) * (size_t)max_seqs + 9 * 16 + items * (sizeof(salt::AttItem) / 4) + T * (sizeof(salt::AttJoin) / 4);
   q->part_rows = (int64_t)(2 * T * (size_t)kv->cfg.n_heads) + salt::kExtraRows;
   if (q->part_rows > INT32_MAX) {
     free_seqs(q);
@@ -628,7 +501,9 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
     const size_t at_slot = at_count + words((size_t)own_refs), at_order = at_slot + words((size_t)T);
     const size_t at_item = at_order + words(w.order.size());
     const size_t at_join = at_item + words(w.items.size() * (sizeof(salt::AttItem) / 4));
-    const size_t total = at_join + w.joins.size() * (sizeof(salt::AttJoin) / 4);
+    const size_t at_seq = at_join + words(w.joins.size() * (sizeof(salt::AttJoin) / 4));
+    const size_t at_rec = at_seq + words((size_t)own_refs);
+    const size_t at_back = at_rec + words((size_t)n * (sizeof(salt::SeqRec) / 4)), total = at_back + (size_t)T;
     if (total > q->words || w.rows > q->part_rows)
       return ctx_fail(ctx, SALT_ERR_BAD_STATE, "%zu words and %lld partial rows exceed the sequences' %zu and %lld",
                       total, (long long)w.rows, q->words, (long long)q->part_rows);
@@ -641,17 +516,25 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
     if (pre_refs) std::memcpy(d + at_page, b->prefix_pages, (size_t)pre_refs * 4);
     if (own_refs) std::memcpy(d + at_page + pre_refs, b->pages, (size_t)own_refs * 4);
     // two tokens of the batch written into one page from two sequences would race
-    bool clash = false;
+    bool clash = false, shared = false;
     if (++kv->stamps == 0) {
       std::fill(kv->stamp.begin(), kv->stamp.end(), 0u);
+      std::fill(kv->held.begin(), kv->held.end(), 0u);
       kv->stamps = 1;
     }
-    int t = 0, row = 0;
+    for (int i = 0; i < nd; ++i)
+      for (int k = 0; k < ceil_div(b->prefix_len[i], pt); ++k)
+        kv->held[(size_t)b->prefix_pages[b->prefix_off[i] + k]] = kv->stamps;
+    int t = 0, row = 0, max_len = 0;
+    salt::SeqRec* rec = reinterpret_cast<salt::SeqRec*>(d + at_rec);
     for (int i = 0; i < n; ++i) {
+      rec[i] = salt::SeqRec{t, b->q_len[i], b->len[i], pre_refs + b->page_off[i]};
+      max_len = std::max(max_len, b->len[i]);
       const int len = b->len[i], first = len - b->q_len[i];
       const int32_t* pages = b->pages + b->page_off[i];
       for (int j = 0; j < b->q_len[i]; ++j, ++t) {
         const int pos = first + j;
+        d[at_back + t] = b->q_len[i] - 1 - j;
         d[at_slot + t] = pos < 0 ? -1 : pages[pos / pt] * pt + pos % pt;
         if (pos >= 0 && (pos % pt == 0 || pos == std::max(first, 0))) {
           uint32_t& st_ = kv->stamp[(size_t)pages[pos / pt]];
@@ -663,6 +546,12 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
         const int k = r - b->page_off[i];
         d[at_row + r] = salt::page_row(row, len, pt, k);
         d[at_count + r] = salt::page_count(len, pt, k);
+        d[at_seq + r] = i;
+        if (d[at_count + r] > 0) {
+          uint32_t& held = kv->held[(size_t)b->pages[r]];
+          shared |= held == kv->stamps;
+          held = kv->stamps;
+        }
       }
       row += len;
     }
@@ -681,6 +570,9 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
     q->n_own_refs = own_refs;
     q->own_tokens = own;
     q->clash = clash;
+    q->shared = shared;
+    q->n_seqs = n;
+    q->max_len = max_len;
     q->at_page = at_page;
     q->at_row = at_row;
     q->at_count = at_count;
@@ -688,6 +580,9 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
     q->at_order = at_order;
     q->at_item = at_item;
     q->at_join = at_join;
+    q->at_seq = at_seq;
+    q->at_rec = at_rec;
+    q->at_back = at_back;
     std::copy(w.n_kind, w.n_kind + 4, q->n_kind);
     q->n_joins = (int)w.joins.size();
   } catch (const std::bad_alloc&) {

@@ -83,6 +83,8 @@ struct KvLayer {
   uint8_t *k, *v;
   float *ks, *vs;
   int32_t kv_heads, dim, log2_page, format;
+  float* weight;            // marks, laid out as the scales (null: not tracked): gathered attention weight, and
+  int32_t* place;           // position of the token
 };
 struct KvWriteArgs {
   KvLayer kv;

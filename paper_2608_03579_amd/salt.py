@@ -32,7 +32,9 @@ EXPORTS = (
     "salt_apply_batch", "salt_apply_batch_noalloc", "salt_apply_batch_timed", "salt_apply_map", "salt_fuse_centroid",
     "salt_fuse_centroid_timed", "salt_adapter_gram", "salt_pin_base", "salt_pin_base_fp8", "salt_read_base",
     "salt_base_product", "salt_kv_bytes", "salt_kv_create", "salt_kv_destroy", "salt_seqs_create", "salt_seqs_destroy",
-    "salt_seqs_set", "salt_kv_write", "salt_kv_read", "salt_attend", "salt_route",
+    "salt_seqs_set", "salt_kv_write", "salt_kv_read", "salt_attend", "salt_rotate", "salt_kv_track",
+    "salt_kv_score", "salt_kv_evict", "salt_kv_read_marks", "salt_kv_write_marks", "salt_beams_create",
+    "salt_beams_destroy", "salt_beam_select", "salt_kv_copy", "salt_route",
     "salt_status_str",
     "salt_last_error", "salt_version",
 )
@@ -60,6 +62,12 @@ class SeqBatch(C.Structure):
                 ("page_off", C.POINTER(C.c_int32)), ("pages", C.POINTER(C.c_int32)),
                 ("domain", C.POINTER(C.c_int32)), ("n_domains", C.c_int32), ("prefix_len", C.POINTER(C.c_int32)),
                 ("prefix_off", C.POINTER(C.c_int32)), ("prefix_pages", C.POINTER(C.c_int32))]
+
+
+class RotationArgs(C.Structure):
+    _fields_ = [("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("rot_dim", C.c_int32),
+                ("interleaved", C.c_int32), ("freq", C.POINTER(C.c_double)), ("q_norm", C.c_void_p),
+                ("k_norm", C.c_void_p), ("eps", C.c_float), ("gain", C.c_float)]
 
 
 class RouteResult(C.Structure):
@@ -112,6 +120,16 @@ def _load() -> C.CDLL:
         "salt_kv_write": (C.c_int, [P, P, I32, VP, C.c_int64, VP, C.c_int64, VP]),
         "salt_kv_read": (C.c_int, [P, P, I32, I32, VP, C.c_int64, VP, C.c_int64, VP]),
         "salt_attend": (C.c_int, [P, P, I32, VP, C.c_int64, VP, C.c_int64, C.c_float, VP]),
+        "salt_rotate": (C.c_int, [P, C.POINTER(RotationArgs), I32, VP] + [VP, C.c_int64] * 4 + [VP]),
+        "salt_kv_track": (C.c_int, [P, P]),
+        "salt_kv_score": (C.c_int, [P, P, I32, VP, C.c_int64, VP, C.c_float, I32, VP]),
+        "salt_kv_evict": (C.c_int, [P, P, I32, I32, I32, VP]),
+        "salt_kv_read_marks": (C.c_int, [P, P, I32, VP, VP, VP]),
+        "salt_kv_write_marks": (C.c_int, [P, P, I32, VP, VP, VP]),
+        "salt_beams_create": (C.c_int, [P, I32, I32, C.POINTER(P)]),
+        "salt_beams_destroy": (None, [P, P]),
+        "salt_beam_select": (C.c_int, [P, P, I32, I32, I32, VP, C.c_int64, VP, I32, VP, VP, VP, VP]),
+        "salt_kv_copy": (C.c_int, [P, P, I32, IP, IP, IP, VP]),
         "salt_route": (C.c_int, [I32] + [C.POINTER(C.c_double)] * 5 + [C.c_double, C.c_double] +
                        [C.POINTER(C.c_double)] * 2 + [C.POINTER(RouteResult)]),
         "salt_status_str": (C.c_char_p, [C.c_int]),
@@ -372,6 +390,25 @@ class Context:
                  fmt: str = "e4m3") -> "KvCache":
         return KvCache(self, n_layers, n_heads, n_kv_heads, head_dim, page_tokens, n_pages, fmt)
 
+    @staticmethod
+    def rotation(n_heads: int, n_kv_heads: int, head_dim: int, freq, interleaved: bool = False, q_norm_ptr: int = 0,
+                 k_norm_ptr: int = 0, eps: float = 1e-6, gain: float = 1.0) -> "Rotation":
+        return Rotation(n_heads, n_kv_heads, head_dim, freq, interleaved, q_norm_ptr, k_norm_ptr, eps, gain)
+
+    def rotate_status(self, rot: "Rotation", T: int, pos_ptr: int, q_ptr: int, q_out_ptr: int, k_ptr: int, k_out_ptr: int,
+                      stream: int = 0, ldq: int = 0, ldqo: int = 0, ldk: int = 0, ldko: int = 0) -> int:
+        return lib.salt_rotate(self.h, C.byref(rot.args), T, pos_ptr, q_ptr, ldq, q_out_ptr, ldqo, k_ptr, ldk, k_out_ptr,
+                               ldko, stream)
+
+    def rotate(self, rot: "Rotation", T: int, pos_ptr: int, q_ptr: int, q_out_ptr: int, k_ptr: int, k_out_ptr: int,
+               stream: int = 0, ldq: int = 0, ldqo: int = 0, ldk: int = 0, ldko: int = 0):
+        """salt_rotate: norms and rotation of q into q_out and k into k_out (in place where they are the same)."""
+        self._check(self.rotate_status(rot, T, pos_ptr, q_ptr, q_out_ptr, k_ptr, k_out_ptr, stream, ldq, ldqo, ldk, ldko),
+                    "salt_rotate")
+
+    def beams(self, max_rows: int, max_out: int) -> "Beams":
+        return Beams(self, max_rows, max_out)
+
     def fuse_centroid_timed(self, table: int, c: int, gamma: float, w_ptr: int, ldw: int, stream: int,
                             start_event: int, stop_event: int):
         """``fuse_centroid`` whose two HIP events record the kernel's own start and end."""
@@ -441,6 +478,47 @@ class Plan:
                     seg_u=seg_u[:n_seg], grp_off=grp_off[:n_grp + 1])
 
 
+class Rotation:
+    """Heads, frequencies (radians per position, one for each rotated pair) and norms of salt_rotate."""
+
+    def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, freq, interleaved: bool = False,
+                 q_norm_ptr: int = 0, k_norm_ptr: int = 0, eps: float = 1e-6, gain: float = 1.0):
+        self.freq = np.ascontiguousarray(freq, dtype=np.float64)
+        self.args = RotationArgs(n_heads, n_kv_heads, head_dim, 2 * len(self.freq), int(interleaved),
+                                 self.freq.ctypes.data_as(C.POINTER(C.c_double)), q_norm_ptr or None, k_norm_ptr or None,
+                                 eps, gain)
+
+
+class Beams:
+    """Scratch of salt_beam_select for up to ``max_rows`` beams of a call and ``max_out`` continuations of a request."""
+
+    def __init__(self, ctx: Context, max_rows: int, max_out: int):
+        self.ctx = ctx
+        h = C.c_void_p()
+        ctx._check(lib.salt_beams_create(ctx.h, max_rows, max_out, C.byref(h)), "salt_beams_create")
+        self._h = h.value
+
+    @property
+    def h(self):
+        return self._h if self.ctx.h else None
+
+    def close(self):
+        if self.h:
+            lib.salt_beams_destroy(self.ctx.h, self.h)
+        self._h = None
+
+    def select_status(self, n_reqs: int, width: int, vocab: int, logits_ptr: int, score_ptr: int, n_out: int,
+                      out_score_ptr: int, out_beam_ptr: int, out_token_ptr: int, stream: int = 0, ld: int = 0) -> int:
+        return lib.salt_beam_select(self.ctx.h, self.h, n_reqs, width, vocab, logits_ptr, ld, score_ptr, n_out,
+                                    out_score_ptr, out_beam_ptr, out_token_ptr, stream)
+
+    def select(self, n_reqs: int, width: int, vocab: int, logits_ptr: int, score_ptr: int, n_out: int,
+               out_score_ptr: int, out_beam_ptr: int, out_token_ptr: int, stream: int = 0, ld: int = 0):
+        """The n_out best continuations of each request: worth, beam and token."""
+        self.ctx._check(self.select_status(n_reqs, width, vocab, logits_ptr, score_ptr, n_out, out_score_ptr, out_beam_ptr,
+                                           out_token_ptr, stream, ld), "salt_beam_select")
+
+
 class KvCache:
     """A paged KV cache in 8 bits (salt_kv): ``fmt`` is "e4m3" or "int8"."""
 
@@ -456,6 +534,21 @@ class KvCache:
     @property
     def nbytes(self) -> int:
         return int(lib.salt_kv_bytes(C.byref(self.cfg)))
+
+    def track(self):
+        """Marks (gathered weight and position) for every token of the cache."""
+        self.ctx._check(lib.salt_kv_track(self.ctx.h, self.h), "salt_kv_track")
+
+    def copy_status(self, src, dst, tokens=None, stream: int = 0) -> int:
+        arrs = [None if a is None else np.ascontiguousarray(a, dtype=np.int32) for a in (src, dst, tokens)]
+        for a in arrs[1:]:
+            if a is not None and len(a) != len(arrs[0]):
+                raise SaltError(ERR_INVALID_ARG, f"{len(a)} entries beside {len(arrs[0])} pages to copy")
+        return lib.salt_kv_copy(self.ctx.h, self.h, len(arrs[0]), *[_i32p(a) for a in arrs], stream)
+
+    def copy(self, src, dst, tokens=None, stream: int = 0):
+        """Pages `dst` become copies of pages `src` (of their first `tokens` tokens) in every layer."""
+        self.ctx._check(self.copy_status(src, dst, tokens, stream), "salt_kv_copy")
 
     def seqs(self, max_seqs: int, max_tokens: int, max_pages: int) -> "Seqs":
         return Seqs(self, max_seqs, max_tokens, max_pages)
@@ -530,3 +623,31 @@ class Seqs:
     def attend(self, layer: int, q_ptr: int, out_ptr: int, scale: float, stream: int = 0, ldq: int = 0, ldo: int = 0):
         """Attention of the step's tokens over the cache."""
         self.ctx._check(self.attend_status(layer, q_ptr, out_ptr, scale, stream, ldq, ldo), "salt_attend")
+
+    def score_status(self, layer: int, q_ptr: int, pos_ptr: int, scale: float, window: int = 0, stream: int = 0,
+                     ldq: int = 0) -> int:
+        return lib.salt_kv_score(self.ctx.h, self.h, layer, q_ptr, ldq, pos_ptr or None, scale, window, stream)
+
+    def score(self, layer: int, q_ptr: int, pos_ptr: int, scale: float, window: int = 0, stream: int = 0, ldq: int = 0):
+        """The attention weight that the step gives to each token, added to its mark."""
+        self.ctx._check(self.score_status(layer, q_ptr, pos_ptr, scale, window, stream, ldq), "salt_kv_score")
+
+    def evict_status(self, layer: int, keep: int, recent: int, stream: int = 0) -> int:
+        return lib.salt_kv_evict(self.ctx.h, self.h, layer, keep, recent, stream)
+
+    def evict(self, layer: int, keep: int, recent: int, stream: int = 0):
+        """Each sequence down to its `keep` tokens of most weight, the `recent` newest positions among them."""
+        self.ctx._check(self.evict_status(layer, keep, recent, stream), "salt_kv_evict")
+
+    def read_marks_status(self, layer: int, weight_ptr: int, pos_ptr: int, stream: int = 0) -> int:
+        return lib.salt_kv_read_marks(self.ctx.h, self.h, layer, weight_ptr, pos_ptr, stream)
+
+    def read_marks(self, layer: int, weight_ptr: int, pos_ptr: int, stream: int = 0):
+        """Gathered weight and position of every own token and kv head."""
+        self.ctx._check(self.read_marks_status(layer, weight_ptr, pos_ptr, stream), "salt_kv_read_marks")
+
+    def write_marks_status(self, layer: int, weight_ptr: int, pos_ptr: int, stream: int = 0) -> int:
+        return lib.salt_kv_write_marks(self.ctx.h, self.h, layer, weight_ptr, pos_ptr, stream)
+
+    def write_marks(self, layer: int, weight_ptr: int, pos_ptr: int, stream: int = 0):
+        self.ctx._check(self.write_marks_status(layer, weight_ptr, pos_ptr, stream), "salt_kv_write_marks")
