@@ -70,7 +70,7 @@ constexpr int kMaxBeams = 64;            // beams of a request, and
 constexpr int kMaxOut = 64;              // continuations: a lane each
 constexpr int kMaxSplits = 64;           // pieces of a row's vocabulary
 constexpr int kMaxBeamRows = 1 << 16, kMaxVocab = 1 << 24;
-constexpr int kSplitVocab = 2048;        // logits of a piece, at least
+constexpr int kSplitVocab = 4096;        // logits of a piece, at least
 // Pieces that the vocabulary of each of `rows` rows is cut into: four blocks to a compute unit, where it has as many.
 inline int beam_splits(int64_t rows, int vocab, int n_cu) {
   const int64_t want = ((int64_t)n_cu * 4 + rows - 1) / std::max<int64_t>(rows, 1);
@@ -82,7 +82,7 @@ struct BeamArgs {
   const void* logits;       // [reqs * width][ld]
   const float* score;       // [reqs * width]
   int64_t ld;
-  uint64_t* best;           // [rows][splits][n_out]: the pieces' best, (order of the value, ~token), 0: none
+  uint64_t* best;           // [rows][n_out][splits]: the pieces' best, (order of the value, ~token), 0: none
   double2* stat;            // [rows][splits]: maximum and sum of exponentials
   float* out_score;         // [reqs][n_out]
   int32_t *out_beam, *out_token;
