@@ -70,17 +70,11 @@ __device__ __forceinline__ uint32_t nth_at_least(uint32_t key, int n) {
   return t;
 }
 
-// The instruction itself: fmaxf first quiets every operand, which might be a signalling NaN.
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
 __device__ __forceinline__ float largest(const float (&v)[16]) {
-  float top = max3(v[0], v[1], v[2]);
+  float top = max3_of(v[0], v[1], v[2]);
 #pragma unroll
-  for (int i = 3; i < 15; i += 2) top = max3(top, v[i], v[i + 1]);
-  return max3(top, v[15], v[15]);
+  for (int i = 3; i < 15; i += 2) top = max3_of(top, v[i], v[i + 1]);
+  return max3_of(top, v[15], v[15]);
 }
 
 // One piece of one row: a block of four waves, which take runs of 1024 logits in turn, 16 to a lane.  A lane's

@@ -97,6 +97,13 @@ __device__ __forceinline__ uint32_t lane_offset(uint32_t v) {
   return v;
 }
 
+// The instruction itself: fmaxf first quiets every operand, which might be a signalling NaN.
+__device__ __forceinline__ float max3_of(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
 template <typename E>
 __device__ __forceinline__ void load8(const E* p, float (&v)[8]) { Ops<E>::to_f32(Ops<E>::load(p), v); }
 

@@ -52,11 +52,12 @@ salt::BatchView view_of(const salt_seqs* q) {
   b.pages = q->dev + q->at_page;
   b.row = q->dev + q->at_row;
   b.count = q->dev + q->at_count;
-  b.seq = q->dev + q->at_seq;
+  b.unit = q->dev + q->at_unit;
   b.rec = reinterpret_cast<const salt::SeqRec*>(q->dev + q->at_rec);
   b.pre_refs = q->n_refs - q->n_own_refs;
   b.own_refs = q->n_own_refs;
   b.n_seqs = q->n_seqs;
+  b.n_units = q->n_units;
   return b;
 }
 
@@ -179,8 +180,10 @@ salt_status salt_kv_score(salt_ctx* ctx, salt_seqs* q, int32_t layer, const void
   const salt_kv* kv = q->kv;
   const int64_t width = (int64_t)kv->cfg.n_heads * kv->cfg.head_dim;
   if ((st = salt::rows_arg(ctx, "q", queries, ldq, width)) != SALT_OK) return st;
+  if (ldq > salt::kScoreRow)
+    return ctx_fail(ctx, SALT_ERR_OUT_OF_RANGE, "q rows of %lld elements, at most %lld", (long long)ldq, (long long)salt::kScoreRow);
   if (reinterpret_cast<uintptr_t>(pos) & 3u) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "misaligned positions");
-  const int64_t blocks = salt::score_blocks(q->n_own_refs, kv->cfg.page_tokens, kv->cfg.n_kv_heads);
+  const int64_t blocks = salt::score_blocks(q->n_units, kv->cfg.n_kv_heads);
   if (blocks > salt::kMaxBlocks)
     return ctx_fail(ctx, SALT_ERR_OUT_OF_RANGE, "the batch takes a launch of %lld blocks, at most %lld", (long long)blocks,
                     (long long)salt::kMaxBlocks);
@@ -207,9 +210,11 @@ salt_status salt_kv_score(salt_ctx* ctx, salt_seqs* q, int32_t layer, const void
   a.pos = pos;
   // (the attention's partial sums of v, which this call has no use for: 2 T heads rows of head_dim floats and more)
   a.fin = reinterpret_cast<float2*>(q->part);
+  a.joined = q->dev + q->at_joined;
   a.window = window == 0 ? INT32_MAX : window;
-  a.T = q->T;
-  a.n_cu = cv.n_cu;
+  const int64_t group = a.att.group;
+  a.few = std::min(q->min_q, a.window) * group <= salt::kFewRows;
+  a.many = std::min(q->max_q, a.window) * group > salt::kFewRows;
   SERVE_HIP(ctx, salt::launch_score(a, cv.bf16, s));
   return SALT_OK;
 }

@@ -32,23 +32,25 @@ hipError_t launch_rotate(const RotateArgs& a, int bf16, int n_cu, hipStream_t s)
 // Arrays of the batch on the device.
 struct BatchView {
   const int32_t* pages;     // page of each reference, the domains' first
-  const int32_t *row, *count, *seq;   // of each own reference: first row of its tokens, tokens, sequence
+  const int32_t *row, *count;         // of each own reference: first row of its tokens, tokens
+  const int32_t* unit;      // sequence of each unit of own keys
   const SeqRec* rec;        // of each sequence
-  int32_t pre_refs, own_refs, n_seqs;
+  int32_t pre_refs, own_refs, n_seqs, n_units;
 };
 struct ScoreArgs {
   AttArgs att;              // as for the attention (v, out and part are not used)
   BatchView b;
   const int32_t* back;      // [T]: new tokens of the sequence behind this one
+  const int32_t* joined;    // [T]: the token's join, or -1: its rows are in one piece
   const int32_t* pos;       // [T], or null: places in the sequence
   float2* fin;              // [T][heads]: maximum (log2) and 1 / sum of a row's logits
-  int32_t window, T, n_cu;
+  int32_t window;
+  int32_t few, many;        // whether the batch has sequences of up to kFewRows counted rows, and of more
 };
-// Keys of a wave's run, and the blocks of the pass that goes by keys.
-constexpr int score_run(int page_tokens) { return page_tokens < 64 ? page_tokens : 64; }
-inline int64_t score_blocks(int64_t own_refs, int page_tokens, int kv_heads) {
-  return (own_refs * (page_tokens / score_run(page_tokens)) + 3) / 4 * kv_heads;
-}
+constexpr int64_t kScoreRow = (int64_t)1 << 24;   // elements between rows of q: 16 of them in 32-bit offsets
+constexpr int kFewRows = 128;            // counted rows of a sequence (for each kv head) that one wave goes through
+// Blocks of the pass that goes by keys, a block to every unit at most.
+inline int64_t score_blocks(int64_t units, int kv_heads) { return units * kv_heads; }
 hipError_t launch_score(const ScoreArgs& a, int bf16, hipStream_t s);
 struct MarksArgs {
   KvLayer kv;

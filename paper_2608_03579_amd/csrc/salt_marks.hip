@@ -8,7 +8,7 @@
 // t over the step's counted tokens that see j, h over the query heads of the kv head, i over all keys that
 // the attention of t reads (prefix and own).  Two passes over the keys: the first finds the maximum and sum of
 // every row (k_score_stat, over the attention's own work items; k_score_join where a row is in pieces),
-// the second goes by keys and adds up exp2(logit - maximum) / sum over the rows (k_score_add): every
+// the second goes by keys and adds up exp2(logit - maximum) / sum over the rows (k_score_few, k_score_many): every
 // mark has one owner and is written once, so no atomics, and the sum's order is fixed.
 // Codes are exact in bf16; q enters as it is in bf16 contexts, in three bf16 terms (24 bits) in fp32 ones.
 #include <hip/hip_runtime.h>
@@ -26,16 +26,17 @@ namespace {
 template <typename E>
 constexpr int terms() { return sizeof(E) == 4 ? 3 : 1; }   // bf16 terms of q
 
-// A query row's values that one lane brings to the products: from dim / 4 g on.
+// A vector's values that lane group g brings to the products are a run of dim / 4 from dim / 4 g on.
 template <typename E, int D>
-__device__ __forceinline__ void load_query(const E* q, bool used, uint4 (&o)[terms<E>()][D / 32]) {
+__device__ __forceinline__ void load_query(const E* q, int g, bool used, uint4 (&o)[terms<E>()][D / 32]) {
 #pragma unroll
   for (int ks = 0; ks < D / 32; ++ks) {
+    const E* at = q + g * (D / 4) + 8 * ks;
     if constexpr (sizeof(E) == 2) {
-      o[0][ks] = used ? *reinterpret_cast<const uint4*>(q + 8 * ks) : make_uint4(0u, 0u, 0u, 0u);
+      o[0][ks] = used ? *reinterpret_cast<const uint4*>(at) : make_uint4(0u, 0u, 0u, 0u);
     } else {
       float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (used) load8(q + 8 * ks, f);
+      if (used) load8(at, f);
       uint4 t[terms<E>()];
       split_terms<terms<E>()>(f, t);
 #pragma unroll
@@ -44,24 +45,49 @@ __device__ __forceinline__ void load_query(const E* q, bool used, uint4 (&o)[ter
   }
 }
 
-// Logits of 16 keys (the lane: keys 4 g + i) and 16 rows (row l & 15), times 1.
-template <typename E, int D, int FMT>
-__device__ __forceinline__ f32x4 logits16(const uint32_t (&k)[D / 16], const uint4 (&q)[terms<E>()][D / 32]) {
-  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+// Rows of kBytes that a wave stages in LDS of its own.  An operand load straight from memory gives neighbouring lanes
+// neighbouring rows: 64 cache lines to an instruction, which the address unit takes a cycle each for (with rows of q
+// read so, k_score_many took 330 us, of which 107 without its loads).  From here the wave reads memory in order,
+// 1 KB to an instruction, and LDS as the operand needs it.  Chunks of 16 bytes change places within their row so
+// that 16 rows' chunks fall into different banks.
+template <int kBytes>
+struct Staged {
+  static constexpr int kChunks = kBytes / 16;              // of a row
+  static constexpr int kRowsAtOnce = 64 / (kChunks < 64 ? kChunks : 64);
+  static __device__ __forceinline__ int at(int row, int chunk) {
+    constexpr int kWindow = kChunks < 16 ? 16 / kChunks : 1;   // rows that 256 bytes hold
+    return row * kBytes + 16 * (chunk ^ ((row / kWindow) & (kChunks - 1) & 15));
+  }
+  // The lane's row and chunk in load j of 64 chunks.
+  static __device__ __forceinline__ int row(int j, int lane) { return (j * 64 + lane) / kChunks; }
+  static __device__ __forceinline__ int chunk(int j, int lane) { return (j * 64 + lane) % kChunks; }
+};
+
+// 16 keys' codes as the products' operand.
+template <int D, int FMT>
+__device__ __forceinline__ void keys_bf16(const uint32_t (&k)[D / 16], uint4 (&o)[D / 32]) {
 #pragma unroll
   for (int ks = 0; ks < D / 32; ++ks) {
     const uint2 lo = codes_bf16<FMT>(k[2 * ks]), hi = codes_bf16<FMT>(k[2 * ks + 1]);
-    const uint4 kb = make_uint4(lo.x, lo.y, hi.x, hi.y);
-#pragma unroll
-    for (int n = 0; n < terms<E>(); ++n) s = mma_bf16(kb, q[n][ks], s);
+    o[ks] = make_uint4(lo.x, lo.y, hi.x, hi.y);
   }
+}
+// Products of 16 keys (the lane: keys 4 g + i) and 16 rows (row l & 15).
+template <typename E, int D>
+__device__ __forceinline__ f32x4 products16(const uint4 (&k)[D / 32], const uint4 (&q)[terms<E>()][D / 32]) {
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int ks = 0; ks < D / 32; ++ks)
+#pragma unroll
+    for (int n = 0; n < terms<E>(); ++n) s = mma_bf16(k[ks], q[n][ks], s);
   return s;
 }
 
-// 32 keys of an item: as the attention has them, without v.
+// 32 keys of an item as they come from memory, 16 and 16 in a row, and through LDS as operands: keys (l & 15) and
+// 16 + (l & 15), a run of dim / 4 codes each.
 template <int D>
 struct Keys32 {
-  uint32_t k[2][D / 16];
+  u32x4 c[2][D / 64];
   float ks[8];
   int end, j0;
   bool own;
@@ -73,15 +99,33 @@ __device__ __forceinline__ void load_keys32(const AttArgs& a, const AttItem& it,
   x.j0 = 32 * (x.own ? step - n_pre : step);
   x.end = x.own ? it.own_end : it.pre_len;
   const int ref = x.own ? it.own_ref : it.pre_ref, last = max(x.end - 1, 0);
-  const int lp = a.kv.log2_page, r = lane & 15, g = lane >> 4;
+  const int lp = a.kv.log2_page, g = lane >> 4;
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     const int j = min(x.j0 + 16 * t, last & ~15);         // a run of 16 keys lies in one page
     const int page = uniform_word(a.pages, ref + (j >> lp));
     const size_t vec = (((size_t)page * a.kv.kv_heads + kvh) << lp) + (j & ((1 << lp) - 1));
-    load_words<D / 16>(a.kv.k + vec * D + lane_offset(r * D + g * (D / 4)), x.k[t]);
+    const uint8_t* k = a.kv.k + vec * D;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) x.c[t][i] = *reinterpret_cast<const u32x4*>(k + lane_offset(i * 1024 + lane * 16));
     const float4 s = *reinterpret_cast<const float4*>(a.kv.ks + vec + (uint32_t)(4 * g));
     x.ks[4 * t] = s.x; x.ks[4 * t + 1] = s.y; x.ks[4 * t + 2] = s.z; x.ks[4 * t + 3] = s.w;
+  }
+}
+// 16 keys into the wave's LDS, and out of it.
+template <int D>
+__device__ __forceinline__ void stage_keys(uint8_t* lds, int lane, const u32x4 (&c)[D / 64]) {
+  using S = Staged<D>;
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) *reinterpret_cast<u32x4*>(lds + S::at(S::row(i, lane), S::chunk(i, lane))) = c[i];
+}
+template <int D>
+__device__ __forceinline__ void read_keys(const uint8_t* lds, int lane, uint32_t (&w)[D / 16]) {
+  const int r = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) {
+    const u32x4 v = *reinterpret_cast<const u32x4*>(lds + Staged<D>::at(r, g * (D / 64) + i));
+    w[4 * i] = v[0]; w[4 * i + 1] = v[1]; w[4 * i + 2] = v[2]; w[4 * i + 3] = v[3];
   }
 }
 
@@ -91,89 +135,142 @@ __device__ __forceinline__ float2 row_final(float m, float l) {
   return make_float2(m == kNegInf ? 0.f : m, l == 0.f ? __builtin_nanf("") : 1.0f / l);
 }
 
-// One item: kWaves = 4: 16 rows, the block's waves take 32 keys in turn; 1: one wave alone.
-// RT > 0 instead: 64 RT rows, 16 RT to a wave, which reads all the item's keys.
-template <typename E, int D, int FMT, int kWaves, int RT>
-__device__ __forceinline__ void stat_item(const ScoreArgs& sa, const AttItem& it, int kvh, float* lds) {
+// One item: RT row tiles of 16 to a wave, WR waves side by side over the rows and WK over the keys, 32 keys in turn.
+// (WK = WR = 1: one wave alone.)  Each lane has a running maximum and sum of its own keys, joined over lanes and
+// waves in the end.  A logit is an fma against the maximum so far, which follows the largest one only when that
+// is kMaxSlack above it.
+template <typename E, int D, int FMT, int RT, int WR, int WK>
+__device__ __forceinline__ void stat_item(const ScoreArgs& sa, const AttItem& it, int kvh, uint8_t* stage, float* lds) {
   const AttArgs& a = sa.att;
-  constexpr int NR = RT > 0 ? RT : 1;
+  constexpr int NT = terms<E>();
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
-  const int wave = kWaves == 1 && RT == 0 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = WR * WK == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wr = wave % WR, wk = wave / WR;
   const int n_pre = 2 * ((it.pre_len + kKeyUnit - 1) / kKeyUnit);
-  const int row0 = RT > 0 ? wave * 16 * RT : 0;
-  if (RT > 0 && row0 >= it.n_rows) return;
-  int st = 2 * it.unit0 + (RT > 0 || kWaves == 1 ? 0 : wave);
-  const int st1 = 2 * it.unit1, by = RT > 0 ? 1 : kWaves;
+  const int row0 = wr * 16 * RT;
+  const bool on = row0 < it.n_rows;                        // (a tile may be short of rows)
+  int st = 2 * it.unit0 + wk;
+  const int st1 = on ? 2 * it.unit1 : 0;
   Keys32<D> x;
   if (st < st1) load_keys32<D>(a, it, n_pre, st, kvh, lane, x);
-  uint4 q[NR][terms<E>()][D / 32];
-  float m[NR], l[NR];
-  int lim[NR];
+  uint4 q[RT][NT][D / 32];
+  float m[RT], l[RT], bar[RT];                             // bar: how far above m a logit may be; -inf: m is not yet set
+  int lim[RT];
 #pragma unroll
-  for (int t = 0; t < NR; ++t) {
+  for (int t = 0; t < RT; ++t) {
     const int row = row0 + 16 * t + r, ti = row / a.group;
     const bool used = row < it.n_rows;
     const int tok = used ? a.order[it.tok0 + ti] : 0;
-    load_query<E, D>(reinterpret_cast<const E*>(a.q) + (size_t)tok * a.ldq + (size_t)(kvh * a.group + row - ti * a.group) * D +
-                         g * (D / 4), used, q[t]);
-    m[t] = kNegInf;
+    load_query<E, D>(reinterpret_cast<const E*>(a.q) + (size_t)tok * a.ldq +
+                               (size_t)(kvh * a.group + row - ti * a.group) * D, g, used, q[t]);
+    m[t] = 0.f;
     l[t] = 0.f;
+    bar[t] = kNegInf;
     lim[t] = it.pos0 + ti + 1;
   }
   const int min_lim = it.pos0 + row0 / a.group + 1;
   const float c = a.scale * kLog2e;
-  while (st < st1) {
-    const int next = st + by;
-    Keys32<D> y;
-    if (next < st1) load_keys32<D>(a, it, n_pre, next, kvh, lane, y);
+  auto use = [&](const Keys32<D>& x) {
     const bool edge = x.j0 + 32 > (x.own ? min_lim : x.end);
+    uint4 k[2][D / 32];
+    float ks[8];
 #pragma unroll
-    for (int t = 0; t < NR; ++t) {
-      float z[8];
+    for (int u = 0; u < 2; ++u) {
+      uint32_t w[D / 16];
+      read_keys<D>(stage + u * 16 * D, lane, w);
+      keys_bf16<D, FMT>(w, k[u]);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ks[e] = x.ks[e] * c;
+    float z[RT][8], top[RT];
+    bool above = false;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const f32x4 s = logits16<E, D, FMT>(x.k[u], q[t]);
+        const f32x4 s = products16<E, D>(k[u], q[t]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) z[4 * u + e] = s[e] * (x.ks[4 * u + e] * c);
+        for (int e = 0; e < 4; ++e) z[t][4 * u + e] = fmaf(s[e], ks[4 * u + e], -m[t]);
       }
-      if (edge) {
+    }
+    if (edge) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
         const int lt = x.own ? min(lim[t], x.end) : x.end;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (x.j0 + 16 * (e >> 2) + 4 * g + (e & 3) >= lt) z[e] = kNegInf;
+          if (x.j0 + 16 * (e >> 2) + 4 * g + (e & 3) >= lt) z[t][e] = kNegInf;
       }
-      const float top = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
-      if (__any(top > m[t] + kMaxSlack)) {                  // (each lane its own maximum)
-        const float mn = fmaxf(m[t], top);
-        l[t] *= m[t] == kNegInf ? 1.f : __builtin_amdgcn_exp2f(m[t] - mn);
-        m[t] = mn;
-      }
-      const float mu = m[t] == kNegInf ? 0.f : m[t];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) l[t] += __builtin_amdgcn_exp2f(z[e] - mu);
     }
-    x = y;
-    st = next;
-  }
 #pragma unroll
-  for (int t = 0; t < NR; ++t) {
+    for (int t = 0; t < RT; ++t) {
+      top[t] = max3_of(max3_of(max3_of(z[t][0], z[t][1], z[t][2]), z[t][3], z[t][4]), max3_of(z[t][5], z[t][6], z[t][7]), z[t][7]);
+      above |= top[t] > bar[t];
+    }
+    if (__any(above)) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        const float up = top[t] > bar[t] ? top[t] : 0.f;
+        if (bar[t] > kNegInf) l[t] *= __builtin_amdgcn_exp2f(-up);
+        if (top[t] > bar[t]) bar[t] = kMaxSlack;
+        m[t] += up;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[t][e] -= up;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) l[t] += __builtin_amdgcn_exp2f(z[t][e]);
+  };
+  auto put = [&](const Keys32<D>& x) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) stage_keys<D>(stage + u * 16 * D, lane, x.c[u]);
+    __builtin_amdgcn_wave_barrier();
+  };
+  Keys32<D> y;
+  for (; st < st1; st += 2 * WK) {
+    put(x);
+    if (st + WK < st1) load_keys32<D>(a, it, n_pre, st + WK, kvh, lane, y);
+    use(x);
+    if (st + WK >= st1) break;
+    put(y);
+    if (st + 2 * WK < st1) load_keys32<D>(a, it, n_pre, st + 2 * WK, kvh, lane, x);
+    use(y);
+  }
+  constexpr int kRows = 16 * RT * WR;
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    if (bar[t] == kNegInf) m[t] = kNegInf;
     const float mr = row_max(m[t]);
     // (a maximum of -inf beside a sum that is not 0: NaN, to be kept)
-    float lr = row_sum(m[t] == kNegInf ? l[t] : l[t] * __builtin_amdgcn_exp2f(m[t] - mr));
-    float mw = mr;
-    if constexpr (RT == 0 && kWaves == 4) {
-      if (g == 0) lds[wave * 16 + r] = mr, lds[64 + wave * 16 + r] = lr;
-      __syncthreads();
-      if (wave) return;
-      mw = fmaxf(fmaxf(lds[r], lds[16 + r]), fmaxf(lds[32 + r], lds[48 + r]));
+    l[t] = row_sum(m[t] == kNegInf ? l[t] : l[t] * __builtin_amdgcn_exp2f(m[t] - mr));
+    m[t] = mr;
+    if constexpr (WK > 1)
+      if (g == 0) {
+        const int at = wk * kRows + row0 + 16 * t + r;
+        lds[at] = m[t];
+        lds[WK * kRows + at] = l[t];
+      }
+  }
+  if constexpr (WK > 1) {
+    __syncthreads();
+    if (wk) return;
+  }
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int row = row0 + 16 * t + r, ti = row / a.group;
+    float mw = m[t], lr = l[t];
+    if constexpr (WK > 1) {
+#pragma unroll
+      for (int w = 1; w < WK; ++w) mw = fmaxf(mw, lds[w * kRows + row]);
       lr = 0.f;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float mi = lds[16 * w + r], li = lds[64 + 16 * w + r];
+      for (int w = 0; w < WK; ++w) {
+        const float mi = lds[w * kRows + row], li = lds[(WK + w) * kRows + row];
         lr += mi == kNegInf ? li : li * __builtin_amdgcn_exp2f(mi - mw);
       }
     }
-    const int row = row0 + 16 * t + r, ti = row / a.group;
     if (g == 0 && row < it.n_rows) {
       if (it.out_row < 0) {
         sa.fin[(size_t)a.order[it.tok0 + ti] * a.heads + kvh * a.group + row - ti * a.group] = row_final(mw, lr);
@@ -184,10 +281,19 @@ __device__ __forceinline__ void stat_item(const ScoreArgs& sa, const AttItem& it
   }
 }
 
+// Row tiles of a wave: what 96 registers of q hold, four at most.
+template <typename E, int D>
+constexpr int row_tiles() {
+  constexpr int n = 96 * 8 / (terms<E>() * D);
+  return n >= 4 ? 4 : n >= 2 ? 2 : 1;
+}
+
 template <typename E, int D, int FMT>
-__global__ void __launch_bounds__(256) k_score_stat(ScoreArgs sa) {
-  __shared__ float lds[128];
+__global__ void __launch_bounds__(256, sizeof(E) * D <= 256 ? 2 : 1) k_score_stat(ScoreArgs sa) {
+  __shared__ float lds[512];
+  __shared__ __attribute__((aligned(16))) uint8_t staged[4][32 * D];
   const AttArgs& a = sa.att;
+  uint8_t* stage = staged[__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)];
   const int n_block = a.n_kind[0] + a.n_kind[1] + a.n_kind[2];
   int item = blockIdx.x / a.kv.kv_heads, kvh = blockIdx.x % a.kv.kv_heads;
   if (item >= n_block) {
@@ -199,13 +305,41 @@ __global__ void __launch_bounds__(256) k_score_stat(ScoreArgs sa) {
   const AttItem& it = a.items[item];
   // a sequence's tile whose tokens all stand before the window
   if (it.pos0 != kAllKeys && sa.back[a.order[it.tok0 + (it.n_rows - 1) / a.group]] >= sa.window) return;
-  if (it.kind == 3) stat_item<E, D, FMT, 1, 0>(sa, it, kvh, lds);
-  else if (it.kind == 0) stat_item<E, D, FMT, 4, 0>(sa, it, kvh, lds);
-  else if (it.kind == 1) stat_item<E, D, FMT, 4, 1>(sa, it, kvh, lds);
-  else if constexpr (attend_rows(sizeof(E), D) == kRowTiles[2]) stat_item<E, D, FMT, 4, 2>(sa, it, kvh, lds);
+  constexpr int RT = row_tiles<E, D>();
+  if (it.kind == 3) stat_item<E, D, FMT, 1, 1, 1>(sa, it, kvh, stage, lds);
+  else if (it.kind == 0) stat_item<E, D, FMT, 1, 1, 4>(sa, it, kvh, stage, lds);
+  else if (it.kind == 1) stat_item<E, D, FMT, RT, 4 / RT, RT>(sa, it, kvh, stage, lds);
+  else if constexpr (attend_rows(sizeof(E), D) == kRowTiles[2]) stat_item<E, D, FMT, RT, 8 / RT, RT / 2>(sa, it, kvh, stage, lds);
 }
 
-// The pieces of a row: 16 lanes per (token, query head).
+// Entry i of p, for a wave-uniform i: by way of the scalar unit.  (p is not written by this launch.)
+template <typename S>
+__device__ __forceinline__ S uniform_entry(const S* p, int i) {
+  constexpr int kWords = sizeof(S) / 4;
+  struct Words {
+    int32_t w[kWords];
+  } v;
+  const auto* w = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(p + __builtin_amdgcn_readfirstlane(i));
+#pragma unroll
+  for (int k = 0; k < kWords; ++k) v.w[k] = w[k];
+  return __builtin_bit_cast(S, v);
+}
+// A joined row's partial result of piece p.
+__device__ __forceinline__ float2 piece_of(const AttArgs& a, const AttJoin& j, int p, int kvh, int hr) {
+  const int k = p >= j.n[0];
+  const size_t row = (size_t)(k ? j.row[1] : j.row[0]) +
+                     (size_t)((k ? p - j.n[0] : p) * a.kv.kv_heads + kvh) * (k ? j.stride[1] : j.stride[0]) +
+                     (k ? j.r0[1] : j.r0[0]) + hr;
+  return *reinterpret_cast<const float2*>(a.stat + 2 * row);
+}
+__device__ __forceinline__ void join_piece(float& m, float& l, float2 st) {
+  const float mn = fmaxf(m, st.x);
+  l = (m == kNegInf ? l : l * __builtin_amdgcn_exp2f(m - mn)) +
+      (st.x == kNegInf ? st.y : st.y * __builtin_amdgcn_exp2f(st.x - mn));
+  m = mn;
+}
+
+// The pieces of a row, for sequences of many rows: 16 lanes per (token, query head).
 __global__ void __launch_bounds__(256) k_score_join(ScoreArgs sa) {
   const AttArgs& a = sa.att;
   const int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
@@ -216,17 +350,7 @@ __global__ void __launch_bounds__(256) k_score_join(ScoreArgs sa) {
   const int h = (int)(i % a.heads), kvh = h / a.group, hr = h - kvh * a.group;
   const int n = j.n[0] + j.n[1];
   float m = kNegInf, l = 0.f;
-  for (int p = lane; p < n; p += 16) {
-    const int k = p >= j.n[0];
-    const size_t row = (size_t)(k ? j.row[1] : j.row[0]) +
-                       (size_t)((k ? p - j.n[0] : p) * a.kv.kv_heads + kvh) * (k ? j.stride[1] : j.stride[0]) +
-                       (k ? j.r0[1] : j.r0[0]) + hr;
-    const float2 st = *reinterpret_cast<const float2*>(a.stat + 2 * row);
-    const float mn = fmaxf(m, st.x);
-    l = (m == kNegInf ? l : l * __builtin_amdgcn_exp2f(m - mn)) +
-        (st.x == kNegInf ? st.y : st.y * __builtin_amdgcn_exp2f(st.x - mn));
-    m = mn;
-  }
+  for (int p = lane; p < n; p += 16) join_piece(m, l, piece_of(a, j, p, kvh, hr));
   float top = m;
 #pragma unroll
   for (int x = 1; x < 16; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
@@ -236,81 +360,290 @@ __global__ void __launch_bounds__(256) k_score_join(ScoreArgs sa) {
   if (lane == 0) sa.fin[(size_t)j.tok * a.heads + h] = row_final(top, l);
 }
 
-// 16 KT keys of one page reference and kv head to a wave, against the counted rows of their sequence that see any.
-template <typename E, int D, int FMT, int KT>
-__global__ void __launch_bounds__(256) k_score_add(ScoreArgs sa, int chunks) {
+// A unit of 64 own keys of one sequence, as one wave has it: bf16 codes and scales times the logits' factor.
+template <int D>
+struct Unit {
+  int j0;                  // place of the first key
+  uint4 k[4][D / 32];
+  float ks[4][4];
+};
+template <int D>
+struct UnitCodes {
+  u32x4 c[4][D / 64];
+  float4 s[4];
+};
+template <int D>
+__device__ __forceinline__ void load_unit(const ScoreArgs& sa, int j0, const SeqRec& rec, int kvh, UnitCodes<D>& x) {
   const AttArgs& a = sa.att;
-  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
-  const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // (the four waves of a block: runs of keys of one kv head, which read the same rows)
-  const int64_t group = w / (4 * a.kv.kv_heads);
-  const int kvh = (int)((w >> 2) % a.kv.kv_heads);
-  const int64_t run = group * 4 + (w & 3);
-  const int ref = (int)(run / chunks), first = (int)(run % chunks) * 16 * KT;
-  if (ref >= sa.b.own_refs) return;
-  const int count = uniform_word(sa.b.count, ref);
-  if (first >= count) return;
-  const SeqRec rec = sa.b.rec[uniform_word(sa.b.seq, ref)];
-  if (rec.q_len == 0) return;
-  const int lp = a.kv.log2_page, G = a.group;
-  const int page = uniform_word(sa.b.pages, sa.b.pre_refs + ref);
-  const int j0 = ((sa.b.pre_refs + ref - rec.ref0) << lp) + first;   // place of the first key in its sequence
-  const size_t vec = (((size_t)page * a.kv.kv_heads + kvh) << lp) + first;
-  uint32_t k[KT][D / 16];
-  float ks[KT][4];
+  const int lane = threadIdx.x & 63, g = lane >> 4, lp = a.kv.log2_page;
+  // the unit's pages, looked up at once: one, or four references in a row (those past the sequence's last are not used)
+  struct Refs {
+    int32_t page[4];
+  } refs{};
+  const int first = rec.ref0 + (j0 >> lp);
+  if (lp >= 6) refs.page[0] = uniform_word(a.pages, first);
+  else refs = uniform_entry(reinterpret_cast<const Refs*>(a.pages + first), 0);
 #pragma unroll
-  for (int t = 0; t < KT; ++t) {
-    load_words<D / 16>(a.kv.k + (vec + 16 * t) * D + lane_offset(r * D + g * (D / 4)), k[t]);
-    const float4 s = *reinterpret_cast<const float4*>(a.kv.ks + vec + 16 * t + 4 * g);
-    const float c = a.scale * kLog2e;
-    ks[t][0] = s.x * c; ks[t][1] = s.y * c; ks[t][2] = s.z * c; ks[t][3] = s.w * c;
+  for (int t = 0; t < 4; ++t) {
+    const int j = min(j0 + 16 * t, (rec.len - 1) & ~15);   // a run of 16 keys lies in one page
+    const int ref = (j >> lp) - (j0 >> lp);
+    const int page = ref == 0 ? refs.page[0] : ref == 1 ? refs.page[1] : ref == 2 ? refs.page[2] : refs.page[3];
+    const size_t vec = (((size_t)page * a.kv.kv_heads + kvh) << lp) + (j & ((1 << lp) - 1));
+    const uint8_t* k = a.kv.k + vec * D;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) x.c[t][i] = *reinterpret_cast<const u32x4*>(k + lane_offset(i * 1024 + lane * 16));
+    x.s[t] = *reinterpret_cast<const float4*>(a.kv.ks + vec + 4 * g);
   }
-  // rows from the first counted token on that sees the first key
-  const int old = rec.len - rec.q_len;
-  const int tok_a = max(max(0, rec.q_len - sa.window), j0 - old);
-  float acc[KT][4] = {};
-  const int rows = (rec.q_len - tok_a) * G;
-  int ti = tok_a + r / G, hr = r % G;
-  const int add_t = 16 / G, add_h = 16 % G;
-  const E* qb = reinterpret_cast<const E*>(a.q) + (size_t)kvh * G * D + g * (D / 4);
-  for (int r0 = 0; r0 < rows; r0 += 16) {
-    const bool used = r0 + r < rows;
-    const size_t tok = (size_t)rec.tok0 + (used ? ti : rec.q_len - 1);
-    uint4 q[terms<E>()][D / 32];
-    load_query<E, D>(qb + tok * a.ldq + (size_t)(used ? hr : 0) * D, used, q);
-    const float2 f = used ? sa.fin[tok * a.heads + kvh * G + hr] : make_float2(0.f, 0.f);
-    const int sees = used ? old + ti - j0 : -1;            // keys 0 .. sees of the run
+}
+template <int D, int FMT>
+__device__ __forceinline__ void convert_unit(const UnitCodes<D>& u, float c, int j0, uint8_t* stage, Unit<D>& x) {
+  const int lane = threadIdx.x & 63;
+  x.j0 = j0;
 #pragma unroll
-    for (int t = 0; t < KT; ++t) {
-      const f32x4 s = logits16<E, D, FMT>(k[t], q);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float p = __builtin_amdgcn_exp2f(s[e] * ks[t][e] - f.x) * f.y;
-        acc[t][e] += 16 * t + 4 * g + e <= sees ? p : 0.f;
-      }
-    }
-    ti += add_t;
-    hr += add_h;
-    if (hr >= G) hr -= G, ++ti;
+  for (int t = 0; t < 4; ++t) {
+    x.ks[t][0] = u.s[t].x * c; x.ks[t][1] = u.s[t].y * c; x.ks[t][2] = u.s[t].z * c; x.ks[t][3] = u.s[t].w * c;
+    uint32_t w[D / 16];
+    stage_keys<D>(stage + (t & 1) * 16 * D, lane, u.c[t]);   // (LDS keeps a wave's order)
+    __builtin_amdgcn_wave_barrier();
+    read_keys<D>(stage + (t & 1) * 16 * D, lane, w);
+    __builtin_amdgcn_wave_barrier();
+    keys_bf16<D, FMT>(w, x.k[t]);
   }
-  // the sum over the row lanes; lane r keeps key 4 g + r % 4 of tile r / 4
+}
+// The first counted token that sees the unit's first key.
+__device__ __forceinline__ int first_token(const ScoreArgs& sa, const SeqRec& rec, int j0) {
+  return max(max(0, rec.q_len - sa.window), j0 - (rec.len - rec.q_len));
+}
+// The sum over the 16 lanes of a row of lanes, in all of them.
+template <int N>
+__device__ __forceinline__ float add_turned(float v) {       // row_ror:N
+  return v + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x120 + N, 0xf, 0xf, true));
+}
+// The weights' sums over the 16 row lanes: lane r gets key 4 g + r % 4 of tile r / 4.
+__device__ __forceinline__ float sum_rows(const float (&acc)[4][4]) {
+  const int r = threadIdx.x & 15;
   float mine = 0.f;
 #pragma unroll
-  for (int t = 0; t < KT; ++t)
+  for (int i = 0; i < 16; ++i) {
+    const float v = add_turned<1>(add_turned<2>(add_turned<4>(add_turned<8>(acc[i >> 2][i & 3]))));
+    mine = r == i ? v : mine;
+  }
+  return mine;
+}
+// Key `at` of the unit has gathered `w` in this step.
+__device__ __forceinline__ void add_mark(const ScoreArgs& sa, const SeqRec& rec, int j, int kvh, float w) {
+  const AttArgs& a = sa.att;
+  if (j >= rec.len) return;
+  const int lp = a.kv.log2_page;
+  const size_t vec = (((size_t)a.pages[rec.ref0 + (j >> lp)] * a.kv.kv_heads + kvh) << lp) + (j & ((1 << lp) - 1));
+  const int fresh = j - (rec.len - rec.q_len);             // (>= 0: the step's own token)
+  const float had = fresh >= 0 ? 0.f : a.kv.weight[vec];
+  a.kv.weight[vec] = had + w;
+  if (fresh >= 0) a.kv.place[vec] = sa.pos ? sa.pos[rec.tok0 + fresh] : j;
+}
+
+// 16 rows against the unit, each key for the rows that see it (kEdge), or for all.
+template <typename E, int D, bool kEdge>
+__device__ __forceinline__ void add_rows(const Unit<D>& x, const uint4 (&q)[terms<E>()][D / 32], float2 f, int sees,
+                                         float (&acc)[4][4]) {
+  const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const f32x4 s = products16<E, D>(x.k[t], q);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      float v = acc[t][e];
-#pragma unroll
-      for (int x = 1; x < 16; x *= 2) v += __shfl_xor(v, x);
-      if (r == 4 * t + e) mine = v;
+      const float p = __builtin_amdgcn_exp2f(fmaf(s[e], x.ks[t][e], -f.x));
+      if (kEdge) acc[t][e] += 16 * t + 4 * g + e <= sees ? p * f.y : 0.f;
+      else acc[t][e] = fmaf(p, f.y, acc[t][e]);
     }
-  const int at = 16 * (r >> 2) + 4 * g + (r & 3);
-  if (r < 4 * KT && first + at < count) {
-    const int j = j0 + at, fresh = j - old;                 // (>= 0: the step's own token)
-    const float had = fresh >= 0 ? 0.f : a.kv.weight[vec + at];
-    a.kv.weight[vec + at] = had + mine;
-    if (fresh >= 0) a.kv.place[vec + at] = sa.pos ? sa.pos[rec.tok0 + fresh] : j;
   }
+}
+
+// Sequences of few counted rows: a wave to a unit and kv head.  The rows' pieces are joined here, by every wave again:
+// a launch less.
+template <typename E, int D, int FMT>
+__global__ void __launch_bounds__(256, sizeof(E) * D <= 256 ? 2 : 1) k_score_few(ScoreArgs sa) {
+  const AttArgs& a = sa.att;
+  __shared__ __attribute__((aligned(16))) uint8_t staged[4][32 * D];
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15, G = a.group;
+  // (the four waves of a block: units of one kv head)
+  const int kvh = blockIdx.x % a.kv.kv_heads;
+  const int unit = (blockIdx.x / a.kv.kv_heads) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (unit >= sa.b.n_units) return;
+  const SeqRec rec = uniform_entry(sa.b.rec, uniform_word(sa.b.unit, unit));
+  if (rec.q_len == 0 || (int64_t)min(rec.q_len, sa.window) * G > kFewRows) return;
+  const int j0 = (unit - rec.unit0) * kKeyUnit, old = rec.len - rec.q_len;
+  UnitCodes<D> codes;
+  load_unit<D>(sa, j0, rec, kvh, codes);
+  int tok_a = __builtin_amdgcn_readfirstlane(first_token(sa, rec, j0));
+  asm volatile("" : "+s"(tok_a));                          // (the keys are on their way before the rest is looked up)
+  const int rows = (rec.q_len - tok_a) * G;
+  // Of a single token the join comes by the scalar unit, which does not wait for the keys.
+  const bool one = rec.q_len - tok_a == 1;
+  int join1 = -1;
+  AttJoin j1{};
+  if (one) {
+    join1 = uniform_word(sa.joined, rec.tok0 + tok_a);
+    if (join1 >= 0) j1 = uniform_entry(a.joins, join1);
+  }
+  Unit<D> x;
+  convert_unit<D, FMT>(codes, a.scale * kLog2e, j0, staged[threadIdx.x >> 6], x);
+  float acc[4][4] = {};
+  const E* qb = reinterpret_cast<const E*>(a.q) + (size_t)kvh * G * D;
+  for (int r0 = 0; r0 < rows; r0 += 16) {
+    const bool used = r0 + r < rows;
+    const int row = used ? r0 + r : 0, ti = tok_a + row / G, hr = row % G;
+    const size_t tok = (size_t)rec.tok0 + ti;
+    uint4 q[terms<E>()][D / 32];
+    load_query<E, D>(qb + tok * a.ldq + (size_t)hr * D, g, used, q);
+    const int join = one ? join1 : sa.joined[tok];
+    const AttJoin j = one ? j1 : join >= 0 ? a.joins[join] : AttJoin{};
+    const int n = join >= 0 ? j.n[0] + j.n[1] : 0;
+    float m = kNegInf, l = 0.f;
+    for (int p = g; p < n; p += 4) join_piece(m, l, piece_of(a, j, p, kvh, hr));   // (a row's four lanes share them)
+    const float top = row_max(m);
+    l = row_sum(m == kNegInf ? l : l * __builtin_amdgcn_exp2f(m - top));
+    const float2 f = join >= 0 ? row_final(top, l) : sa.fin[tok * a.heads + kvh * G + hr];
+    add_rows<E, D, true>(x, q, f, used ? old + ti - x.j0 : -1, acc);
+  }
+  const float w = sum_rows(acc);
+  add_mark(sa, rec, x.j0 + 16 * (r >> 2) + 4 * g + (r & 3), kvh, w);
+}
+
+// Sequences of many counted rows: a block to a unit and kv head, whose waves take 16 rows in turn, the next ones on
+// their way; their sums meet in LDS.
+template <typename E, int D, int FMT>
+__global__ void __launch_bounds__(256, sizeof(E) * D <= 256 ? 2 : 1) k_score_many(ScoreArgs sa) {
+  const AttArgs& a = sa.att;
+  using S = Staged<D * sizeof(E)>;
+  constexpr int kStage = 16 * D * (int)sizeof(E);          // 16 rows, or 32 keys
+  __shared__ __attribute__((aligned(16))) uint8_t staged[4][kStage];
+  __shared__ float sums[4][kKeyUnit];
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15, G = a.group;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint8_t* stage = staged[wave];
+  const int kvh = blockIdx.x % a.kv.kv_heads, unit = blockIdx.x / a.kv.kv_heads;
+  const SeqRec rec = uniform_entry(sa.b.rec, uniform_word(sa.b.unit, unit));
+  if (rec.q_len == 0 || (int64_t)min(rec.q_len, sa.window) * G <= kFewRows) return;
+  const int j0 = (unit - rec.unit0) * kKeyUnit;
+  UnitCodes<D> codes;
+  load_unit<D>(sa, j0, rec, kvh, codes);
+  Unit<D> x;
+  convert_unit<D, FMT>(codes, a.scale * kLog2e, j0, stage, x);
+  const int old = rec.len - rec.q_len, tok_a = first_token(sa, rec, j0);
+  float acc[4][4] = {};
+  // A tile is as many whole tokens as have 16 rows (of groups above 16: a token's rows 16 at a time), so that a lane's
+  // rows lie at fixed offsets from the tile's first.  The last ones first: blocks of all units that run at a time then
+  // read the same rows, which stay in the L2 cache.
+  const int toks = rec.q_len - tok_a;
+  const int per = G <= 16 ? 16 / G : 1, parts = G <= 16 ? 1 : (G + 15) / 16;
+  const int tiles = (toks + per - 1) / per * parts, full = toks / per * parts;
+  // tokens that do not see the unit's last key, and the first tile without any of them
+  const int some = min(max(j0 + kKeyUnit - 1 - old - tok_a, 0), toks);
+  const int plain = min(full, (some + per - 1) / per * parts);
+  const char* qb = reinterpret_cast<const char*>(reinterpret_cast<const E*>(a.q) + ((size_t)rec.tok0 + tok_a) * a.ldq + (size_t)kvh * G * D);
+  const float2* fb = sa.fin + ((size_t)rec.tok0 + tok_a) * a.heads + kvh * G;
+  const uint32_t row_bytes = D * sizeof(E), tok_bytes = (uint32_t)a.ldq * (uint32_t)sizeof(E);   // (ldq <= kScoreRow)
+  // row k of a tile of `n` rows whose heads begin at h0: its token and head
+  auto place = [&](int k, int n, int h0, int& ti, int& hr) {
+    k = min(k, n - 1);
+    ti = G <= 16 ? k / G : 0;
+    hr = G <= 16 ? k - ti * G : h0 + k;
+  };
+  uint32_t off[S::kChunks / 4], f_off;
+  int my_ti = 0;
+  auto offsets = [&](int n, int h0) {
+    int ti, hr;
+#pragma unroll
+    for (int k = 0; k < S::kChunks / 4; ++k) {
+      place(S::row(k, lane), n, h0, ti, hr);
+      off[k] = ti * tok_bytes + hr * row_bytes + 16 * S::chunk(k, lane);
+    }
+    place(r, n, h0, ti, hr);
+    f_off = ti * a.heads + hr;
+    my_ti = ti;
+  };
+  u32x4 c[S::kChunks / 4];                                 // the next tile's rows, on their way
+  float2 f_next;
+  int n_rows = per * G;                                    // of a whole tile; `offsets` are set for it
+  auto first_of = [&](int i) { return G <= 16 ? i * per : i / parts; };   // (from tok_a on)
+  auto load = [&](int i) {
+    const int first = first_of(i);
+    if (G > 16) {
+      const int h0 = (i - first * parts) * 16;
+      n_rows = min(16, G - h0);
+      offsets(n_rows, h0);
+    }
+    const char* base = qb + (size_t)first * tok_bytes;
+#pragma unroll
+    for (int k = 0; k < S::kChunks / 4; ++k) c[k] = *reinterpret_cast<const u32x4*>(base + off[k]);
+    f_next = fb[(size_t)first * a.heads + f_off];
+    if (r >= n_rows) f_next = make_float2(__builtin_inff(), 0.f);   // (exp2(-inf) * 0)
+  };
+  auto put = [&]() {
+#pragma unroll
+    for (int k = 0; k < S::kChunks / 4; ++k)
+      *reinterpret_cast<u32x4*>(stage + S::at(S::row(k, lane), S::chunk(k, lane))) = c[k];
+    __builtin_amdgcn_wave_barrier();
+  };
+  auto take = [&](uint4 (&q)[terms<E>()][D / 32]) {
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks) {
+      constexpr int kEach = sizeof(E) / 2;                 // chunks of 8 values
+      u32x4 v[kEach];
+#pragma unroll
+      for (int u = 0; u < kEach; ++u)
+        v[u] = *reinterpret_cast<const u32x4*>(stage + S::at(r, (g * (D / 32) + ks) * kEach + u));
+      if constexpr (sizeof(E) == 2) {
+        q[0][ks] = make_uint4(v[0][0], v[0][1], v[0][2], v[0][3]);
+      } else {
+        const float w[8] = {__uint_as_float(v[0][0]), __uint_as_float(v[0][1]), __uint_as_float(v[0][2]), __uint_as_float(v[0][3]),
+                            __uint_as_float(v[1][0]), __uint_as_float(v[1][1]), __uint_as_float(v[1][2]), __uint_as_float(v[1][3])};
+        uint4 t[terms<E>()];
+        split_terms<terms<E>()>(w, t);
+#pragma unroll
+        for (int n = 0; n < terms<E>(); ++n) q[n][ks] = t[n];
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  };
+  uint4 q[terms<E>()][D / 32];
+  if (full < tiles && wave == (full & 3)) {                // the tile that is short of tokens
+    n_rows = (toks - full * per) * G;
+    offsets(n_rows, 0);
+    load(full);
+    put();
+    take(q);
+    add_rows<E, D, true>(x, q, f_next, r < n_rows ? old + tok_a + full * per + my_ti - j0 : -1, acc);
+    n_rows = per * G;
+  }
+  int i = ((full - 1 - wave) & ~3) + wave;                 // (the wave's last whole tile; below 0: it has none)
+  if (i >= 0) {
+    offsets(n_rows, 0);
+    load(i);
+    put();
+  }
+  // a tile's rows leave LDS, the next tile's go there from the registers they came to, and those of the one after set out
+  for (; i >= plain; i -= 4) {
+    const float2 f = f_next;
+    take(q);
+    if (i >= 4) load(i - 4);
+    add_rows<E, D, false>(x, q, f, 0, acc);
+    if (i >= 4) put();
+  }
+  for (; i >= 0; i -= 4) {
+    const float2 f = f_next;
+    const int sees = r < n_rows ? old + tok_a + first_of(i) + my_ti - j0 : -1;
+    take(q);
+    if (i >= 4) load(i - 4);
+    add_rows<E, D, true>(x, q, f, sees, acc);
+    if (i >= 4) put();
+  }
+  sums[wave][16 * (r >> 2) + 4 * g + (r & 3)] = sum_rows(acc);
+  __syncthreads();
+  if (threadIdx.x < kKeyUnit)
+    add_mark(sa, rec, x.j0 + threadIdx.x, kvh,
+             (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]));
 }
 
 // Marks out of the cache or into it: a block takes one page reference.
@@ -495,18 +828,14 @@ void score_typed(const ScoreArgs& sa, hipStream_t s) {
   const AttArgs& a = sa.att;
   const int blocks = (a.n_kind[0] + a.n_kind[1] + a.n_kind[2]) * a.kv.kv_heads + cdiv(a.n_kind[3] * a.kv.kv_heads, 4);
   hipLaunchKernelGGL((k_score_stat<E, D, FMT>), dim3(blocks), dim3(256), 0, s, sa);
-  if (a.n_joins)
+  if (a.n_joins && sa.many)
     hipLaunchKernelGGL(k_score_join, dim3((unsigned)(((int64_t)a.n_joins * a.heads + 15) / 16)), dim3(256), 0, s, sa);
-  auto add = [&](auto kt) {
-    constexpr int KT = decltype(kt)::value;
-    if (sa.b.own_refs == 0) return;
-    const int page = 1 << a.kv.log2_page;
-    hipLaunchKernelGGL((k_score_add<E, D, FMT, KT>), dim3((unsigned)score_blocks(sa.b.own_refs, page, a.kv.kv_heads)),
-                       dim3(256), 0, s, sa, page / score_run(page));
-  };
-  if (score_run(1 << a.kv.log2_page) == 16) add(std::integral_constant<int, 1>());
-  else if (score_run(1 << a.kv.log2_page) == 32) add(std::integral_constant<int, 2>());
-  else add(std::integral_constant<int, 4>());
+  const int units = sa.b.n_units;
+  if (units && sa.many)
+    hipLaunchKernelGGL((k_score_many<E, D, FMT>), dim3((unsigned)score_blocks(units, a.kv.kv_heads)), dim3(256), 0, s, sa);
+  if (units && sa.few)
+    hipLaunchKernelGGL((k_score_few<E, D, FMT>), dim3((unsigned)score_blocks((units + 3) / 4, a.kv.kv_heads)), dim3(256), 0, s,
+                       sa);
 }
 template <typename E, int D>
 void score_format(const ScoreArgs& a, hipStream_t s) {

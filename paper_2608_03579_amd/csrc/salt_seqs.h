@@ -47,10 +47,15 @@ struct AttJoin {
   int32_t pad_;
 };
 
-// A sequence of the batch: its first row of q, its new and its own tokens, its first page reference.
+// A sequence of the batch: its first row of q, its new and its own tokens, its first page reference, and the first of
+// its units of kKeyUnit own keys.
 struct SeqRec {
-  int32_t tok0, q_len, len, ref0;
+  int32_t tok0, q_len, len, ref0, unit0, pad_[3];
 };
+// Units that `pages` page references can hold.
+constexpr int64_t most_units(int64_t pages, int page_tokens) {
+  return pages * (page_tokens > kKeyUnit ? page_tokens / kKeyUnit : 1);
+}
 
 struct SeqBatch {
   int n_seqs, n_domains;

@@ -387,8 +387,9 @@ salt_status salt_seqs_create(salt_ctx* ctx, salt_kv* kv, int32_t max_seqs, int32
   q->max_pages = max_pages;
   const size_t T = (size_t)max_tokens;
   const size_t items = (size_t)salt::attend_max_items(max_tokens, kv->cfg.n_heads);
-  // (each of the nine arrays behind the first starts at a multiple of 16 words)
-  q->words = 4 * (size_t)max_pages + 4 * T + (sizeof(salt::SeqRec) / 4) * (size_t)max_seqs + 9 * 16 + items * (sizeof(salt::AttItem) / 4) + T * (sizeof(salt::AttJoin) / 4);
+  // (each of the ten arrays behind the first starts at a multiple of 16 words)
+  q->words = 3 * (size_t)max_pages + (size_t)salt::most_units(max_pages, kv->cfg.page_tokens) + 5 * T +
+             (sizeof(salt::SeqRec) / 4) * (size_t)max_seqs + 10 * 16 + items * (sizeof(salt::AttItem) / 4) + T * (sizeof(salt::AttJoin) / 4);
   q->part_rows = (int64_t)(2 * T * (size_t)kv->cfg.n_heads) + salt::kExtraRows;
   if (q->part_rows > INT32_MAX) {
     free_seqs(q);
@@ -501,9 +502,12 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
     const size_t at_slot = at_count + words((size_t)own_refs), at_order = at_slot + words((size_t)T);
     const size_t at_item = at_order + words(w.order.size());
     const size_t at_join = at_item + words(w.items.size() * (sizeof(salt::AttItem) / 4));
-    const size_t at_seq = at_join + words(w.joins.size() * (sizeof(salt::AttJoin) / 4));
-    const size_t at_rec = at_seq + words((size_t)own_refs);
-    const size_t at_back = at_rec + words((size_t)n * (sizeof(salt::SeqRec) / 4)), total = at_back + (size_t)T;
+    int64_t n_units = 0;
+    for (int i = 0; i < n; ++i) n_units += ceil_div(b->len[i], salt::kKeyUnit);
+    const size_t at_unit = at_join + words(w.joins.size() * (sizeof(salt::AttJoin) / 4));
+    const size_t at_rec = at_unit + words((size_t)n_units);
+    const size_t at_back = at_rec + words((size_t)n * (sizeof(salt::SeqRec) / 4));
+    const size_t at_joined = at_back + words((size_t)T), total = at_joined + (size_t)T;
     if (total > q->words || w.rows > q->part_rows)
       return ctx_fail(ctx, SALT_ERR_BAD_STATE, "%zu words and %lld partial rows exceed the sequences' %zu and %lld",
                       total, (long long)w.rows, q->words, (long long)q->part_rows);
@@ -525,11 +529,14 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
     for (int i = 0; i < nd; ++i)
       for (int k = 0; k < ceil_div(b->prefix_len[i], pt); ++k)
         kv->held[(size_t)b->prefix_pages[b->prefix_off[i] + k]] = kv->stamps;
-    int t = 0, row = 0, max_len = 0;
+    int t = 0, row = 0, max_len = 0, unit = 0, min_q = 0, max_q = 0;
     salt::SeqRec* rec = reinterpret_cast<salt::SeqRec*>(d + at_rec);
     for (int i = 0; i < n; ++i) {
-      rec[i] = salt::SeqRec{t, b->q_len[i], b->len[i], pre_refs + b->page_off[i]};
+      rec[i] = salt::SeqRec{t, b->q_len[i], b->len[i], pre_refs + b->page_off[i], unit, {0, 0, 0}};
       max_len = std::max(max_len, b->len[i]);
+      max_q = std::max(max_q, b->q_len[i]);
+      if (b->q_len[i] > 0) min_q = min_q ? std::min(min_q, b->q_len[i]) : b->q_len[i];
+      for (int u = ceil_div(b->len[i], salt::kKeyUnit); u > 0; --u) d[at_unit + unit++] = i;
       const int len = b->len[i], first = len - b->q_len[i];
       const int32_t* pages = b->pages + b->page_off[i];
       for (int j = 0; j < b->q_len[i]; ++j, ++t) {
@@ -546,7 +553,6 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
         const int k = r - b->page_off[i];
         d[at_row + r] = salt::page_row(row, len, pt, k);
         d[at_count + r] = salt::page_count(len, pt, k);
-        d[at_seq + r] = i;
         if (d[at_count + r] > 0) {
           uint32_t& held = kv->held[(size_t)b->pages[r]];
           shared |= held == kv->stamps;
@@ -557,6 +563,8 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
     }
     std::memcpy(d + at_order, w.order.data(), w.order.size() * 4);
     if (!w.items.empty()) std::memcpy(d + at_item, w.items.data(), w.items.size() * sizeof(salt::AttItem));
+    std::fill(d + at_joined, d + at_joined + T, -1);
+    for (size_t j = 0; j < w.joins.size(); ++j) d[at_joined + w.joins[j].tok] = (int32_t)j;
     if (!w.joins.empty()) std::memcpy(d + at_join, w.joins.data(), w.joins.size() * sizeof(salt::AttJoin));
     if ((st = enter_stream(ctx, q->order, s)) != SALT_OK) return st;
     if (total > 0) {
@@ -580,7 +588,11 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
     q->at_order = at_order;
     q->at_item = at_item;
     q->at_join = at_join;
-    q->at_seq = at_seq;
+    q->at_unit = at_unit;
+    q->at_joined = at_joined;
+    q->n_units = unit;
+    q->min_q = min_q;
+    q->max_q = max_q;
     q->at_rec = at_rec;
     q->at_back = at_back;
     std::copy(w.n_kind, w.n_kind + 4, q->n_kind);

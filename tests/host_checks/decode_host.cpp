@@ -276,12 +276,14 @@ static int launches() {
     const salt::BatchView& b = g_score.b;
     need(b.pre_refs == 1 && b.own_refs == 5 && b.n_seqs == 2, "references", b.pre_refs, b.own_refs);
     for (int i = 0; i < 5; ++i) {
-      const int seq = i < 3 ? 0 : 1, count[5] = {16, 16, 8, 16, 1}, row[5] = {0, 16, 32, 40, 56};
-      need(b.seq[i] == seq && b.count[i] == count[i] && b.row[i] == row[i] && b.pages[1 + i] == pages[i], "reference", i);
+      const int count[5] = {16, 16, 8, 16, 1}, row[5] = {0, 16, 32, 40, 56};
+      need(b.count[i] == count[i] && b.row[i] == row[i] && b.pages[1 + i] == pages[i], "reference", i);
     }
     need(b.pages[0] == 11, "the prefix' page");
     need(b.rec[0].tok0 == 0 && b.rec[0].q_len == 1 && b.rec[0].len == 40 && b.rec[0].ref0 == 1, "record 0");
     need(b.rec[1].tok0 == 1 && b.rec[1].q_len == 2 && b.rec[1].len == 17 && b.rec[1].ref0 == 4, "record 1");
+    need(b.n_units == 2 && b.unit[0] == 0 && b.unit[1] == 1 && b.rec[0].unit0 == 0 && b.rec[1].unit0 == 1, "units");
+    need(g_score.joined[0] == -1 && g_score.joined[2] == -1 && g_score.few && !g_score.many, "joins and rows");
     need(g_score.back[0] == 0 && g_score.back[1] == 1 && g_score.back[2] == 0, "tokens behind");
     need(g_score.window == INT32_MAX, "window 0: all");
     int n = g_launches;
