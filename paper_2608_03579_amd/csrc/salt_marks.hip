@@ -670,31 +670,219 @@ __global__ void __launch_bounds__(256) k_marks(MarksArgs a) {
 // One (sequence, kv head) to a block.  Of n > keep tokens those stay that come first by: position among the
 // `recent` newest; weight, larger ones first, NaN above all; place, lower ones first.  The number that a token
 // orders by is 32 bits wide; a radix select (11, 11 and 10 bits, histograms in LDS) finds the keep-th
-// largest, a bit for each token says which stay, and the kept ones behind place `keep` go to
-// the places of the dropped ones before it, in order.  No two moves touch one place.
+// largest, and the kept ones behind place `keep` go to the places of the dropped ones before it, in order.
+// No two moves touch one place.  A block's chain of steps bounds it, not the bytes: up to kEvictShort tokens have
+// their marks read once, into registers (k_evict); longer sequences go through memory again in each step (k_evict_long).
 constexpr uint32_t kProtected = 0xffffffffu, kNanKey = 0xfffffffeu;
 __device__ __forceinline__ uint32_t weight_order(float w) {
   if (w != w) return kNanKey;
   const uint32_t u = __float_as_uint(w + 0.f);             // (-0 is 0)
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-constexpr int kBins = 2048, kMoves = 2048;                 // moves listed at a time
+constexpr int kBins = 2048;
+constexpr int kEvictShort = 16 * 1024, kPageCache = kEvictShort / 16;
 
-struct alignas(16) EvictLds {                                          // dynamic LDS: keys (kept where they fit), bits, and these
+// From `hist`, counts of digits: the digit that the `need`-th largest key has, and its rank among those.  All threads
+// call it; kWaves waves, whose totals are in `wave`.
+template <int kWaves>
+__device__ __forceinline__ void find_digit(const uint32_t* hist, uint32_t* wave, uint32_t* found, int need) {
+  constexpr int kEach = kBins / (64 * kWaves);             // bins of a lane, the largest digits in the first lane
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  uint32_t c[kEach], sum = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) sum += c[i] = hist[kBins - 1 - (tid * kEach + i)];
+  uint32_t upto = sum;
+#pragma unroll
+  for (int i = 1; i < 64; i *= 2) {
+    const uint32_t o = __shfl_up(upto, i);
+    upto += lane >= i ? o : 0u;
+  }
+  if (lane == 63) wave[wv] = upto;
+  __syncthreads();
+  uint32_t before = upto - sum;
+  for (int i = 0; i < wv; ++i) before += wave[i];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    if (before < (uint32_t)need && before + c[i] >= (uint32_t)need) {
+      found[0] = kBins - 1 - (tid * kEach + i);
+      found[1] = (uint32_t)need - before;
+    }
+    before += c[i];
+  }
+  __syncthreads();
+}
+
+struct alignas(16) EvictLds {
+  union {
+    uint32_t hist[kBins];
+    uint32_t count[kEvictShort / 64];                      // of each 64 places
+  };
+  uint32_t wave[16], found[2];
+  int32_t newest;
+  uint16_t hole[kEvictShort / 2], mover[kEvictShort / 2];
+};
+
+template <int NT, int IT>   // threads, tokens of each
+__global__ void __launch_bounds__(NT) k_evict(EvictArgs a) {
+  constexpr int kItems = IT;
+  __shared__ EvictLds sh;
+  __shared__ int32_t s_page[kPageCache];
+  constexpr int kWaves = NT / 64, kWords = kItems * kWaves;
+  const int seq = blockIdx.x / a.kv.kv_heads, kvh = blockIdx.x % a.kv.kv_heads;
+  const SeqRec rec = a.b.rec[seq];
+  const int n = rec.len, keep = a.keep, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  if (n <= keep) return;
+  const int lp = a.kv.log2_page, hk = a.kv.kv_heads;
+  for (int i = tid; i <= (n - 1) >> lp; i += NT) s_page[i] = a.b.pages[rec.ref0 + i];
+  if (tid == 0) sh.newest = INT32_MIN;
+  for (int i = tid; i < kBins; i += NT) sh.hist[i] = 0;
+  __syncthreads();
+  auto vec_of = [&](int j) { return (((size_t)s_page[j >> lp] * hk + kvh) << lp) + (j & ((1 << lp) - 1)); };
+  // token it * NT + tid in item `it`: a wave has 64 places in a row
+  uint32_t key[kItems];
+  {
+    float w[kItems];
+    int p[kItems];
+    int top = INT32_MIN;
+#pragma unroll
+    for (int it = 0; it < kItems; ++it) {
+      const size_t v = vec_of(min(it * NT + tid, n - 1));  // (past the last token: that one again)
+      w[it] = a.kv.weight[v];
+      p[it] = a.kv.place[v];
+    }
+#pragma unroll
+    for (int it = 0; it < kItems; ++it) {
+      top = max(top, p[it]);
+    }
+    for (int i = 1; i < 64; i *= 2) top = max(top, __shfl_xor(top, i));
+    if (lane == 0) atomicMax(&sh.newest, top);
+    __syncthreads();
+    const int64_t since = (int64_t)sh.newest - a.recent;
+#pragma unroll
+    for (int it = 0; it < kItems; ++it) {
+      key[it] = a.recent > 0 && (int64_t)p[it] > since ? kProtected : weight_order(w[it]);
+    }
+  }
+  // the keep-th largest key: `prefix`, of which `need` stay
+  uint32_t prefix = 0;
+  int need = keep;
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
+#pragma unroll
+    for (int it = 0; it < kItems; ++it) {
+      if (it * NT + tid < n && (pass == 0 || (key[it] >> (shift + width)) == (prefix >> (shift + width))))
+        atomicAdd(&sh.hist[(key[it] >> shift) & ((1u << width) - 1u)], 1u);
+    }
+    __syncthreads();
+    find_digit<kWaves>(sh.hist, sh.wave, sh.found, need);
+    prefix |= sh.found[0] << shift;
+    need = (int)sh.found[1];
+    for (int i = tid; i < kBins; i += NT) sh.hist[i] = 0;
+    __syncthreads();
+  }
+  // Sums over the 64-place words before each word, in order: by wave 0, whose lanes have kWords / 64 words each.
+  auto scan = [&]() {
+    __syncthreads();
+    if (wv == 0) {
+      constexpr int kEach = (kWords + 63) / 64;
+      uint32_t c[kEach], sum = 0;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) sum += c[i] = lane * kEach + i < kWords ? sh.count[lane * kEach + i] : 0u;
+      uint32_t upto = sum;
+#pragma unroll
+      for (int i = 1; i < 64; i *= 2) {
+        const uint32_t o = __shfl_up(upto, i);
+        upto += lane >= i ? o : 0u;
+      }
+      uint32_t before = upto - sum;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        if (lane * kEach + i < kWords) sh.count[lane * kEach + i] = before;
+        before += c[i];
+      }
+      if (lane == 63) sh.found[0] = before;
+    }
+    __syncthreads();
+  };
+  const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+  for (int it = 0; it < kItems; ++it) {
+    const uint64_t same = __ballot(it * NT + tid < n && key[it] == prefix);
+    if (lane == 0) sh.count[it * kWaves + wv] = (uint32_t)__popcll(same);
+  }
+  scan();
+  uint32_t stays = 0;                                      // bit `it`
+  uint32_t mine[kItems];                                   // holes in the lower half, movers in the upper one
+#pragma unroll
+  for (int it = 0; it < kItems; ++it) {
+    const int j = it * NT + tid;
+    const uint64_t same = __ballot(j < n && key[it] == prefix);
+    const int rank = (int)sh.count[it * kWaves + wv] + __popcll(same & below);
+    const bool s = j < n && (key[it] > prefix || (key[it] == prefix && rank < need));
+    stays |= (uint32_t)s << it;
+    mine[it] = (uint32_t)__popcll(__ballot(j < keep && !s)) | ((uint32_t)__popcll(__ballot(j >= keep && s)) << 16);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int it = 0; it < kItems; ++it) {
+    if (lane == 0) sh.count[it * kWaves + wv] = mine[it];
+  }
+  scan();
+#pragma unroll
+  for (int it = 0; it < kItems; ++it) {
+    const int j = it * NT + tid;
+    const bool s = (stays >> it) & 1;
+    const uint32_t before = sh.count[it * kWaves + wv];
+    const uint64_t hs = __ballot(j < keep && !s), ms = __ballot(j >= keep && s);
+    if (j < keep && !s) sh.hole[(before & 0xffffu) + __popcll(hs & below)] = (uint16_t)j;
+    if (j >= keep && s) sh.mover[(before >> 16) + __popcll(ms & below)] = (uint16_t)j;
+  }
+  __syncthreads();
+  const int total = (int)(sh.found[0] & 0xffffu), dv = a.kv.dim / 16;   // (as many movers)
+  const int log_dv = 31 - __builtin_clz(dv);
+  for (int i0 = tid; i0 < total * 2 * dv; i0 += 4 * NT) {
+    u32x4 c[4];
+    uint8_t* to[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + u * NT;
+      if (i >= total * 2 * dv) continue;
+      const int mv = i >> (log_dv + 1), part = i & (2 * dv - 1);
+      uint8_t* p = part < dv ? a.kv.k : a.kv.v;
+      const int o = (part & (dv - 1)) * 16;
+      c[u] = *reinterpret_cast<const u32x4*>(p + vec_of(sh.mover[mv]) * a.kv.dim + o);
+      to[u] = p + vec_of(sh.hole[mv]) * a.kv.dim + o;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i0 + u * NT < total * 2 * dv) *reinterpret_cast<u32x4*>(to[u]) = c[u];
+  }
+  for (int i = tid; i < total; i += NT) {
+    const size_t from = vec_of(sh.mover[i]), to = vec_of(sh.hole[i]);
+    const float ks = a.kv.ks[from], vs = a.kv.vs[from], w = a.kv.weight[from];
+    const int p = a.kv.place[from];
+    a.kv.ks[to] = ks;
+    a.kv.vs[to] = vs;
+    a.kv.weight[to] = w;
+    a.kv.place[to] = p;
+  }
+}
+
+// The same for longer sequences: a bit for each token in LDS says which stay, and moves are listed kMoves at a time.
+constexpr int kMoves = 2048;
+struct alignas(16) EvictLongLds {                          // dynamic LDS: these, and the bits
   uint32_t hist[kBins];
   int32_t hole[kMoves], mover[kMoves];
   int32_t wave[16], wave2[16];
+  uint32_t digits[16], found[2];
   int32_t newest;
-  uint32_t prefix;
-  int32_t need;
 };
 
-template <int NT>   // threads
-__global__ void __launch_bounds__(NT) k_evict(EvictArgs a, int cached) {
+__global__ void __launch_bounds__(1024) k_evict_long(EvictArgs a) {
+  constexpr int NT = 1024;
   extern __shared__ __attribute__((aligned(16))) char dyn[];
-  EvictLds& sh = *reinterpret_cast<EvictLds*>(dyn);
-  uint32_t* bits = reinterpret_cast<uint32_t*>(dyn + sizeof(EvictLds));
-  uint32_t* keys = bits + (a.max_len + 63) / 64 * 2;       // (cached: room for max_len keys)
+  EvictLongLds& sh = *reinterpret_cast<EvictLongLds*>(dyn);
+  uint32_t* bits = reinterpret_cast<uint32_t*>(dyn + sizeof(EvictLongLds));
   const int seq = blockIdx.x / a.kv.kv_heads, kvh = blockIdx.x % a.kv.kv_heads;
   const SeqRec rec = a.b.rec[seq];
   const int n = rec.len, keep = a.keep, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
@@ -714,14 +902,11 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs a, int cached) {
     __syncthreads();
   }
   const int64_t since = a.recent > 0 ? (int64_t)sh.newest - a.recent : INT64_MAX;
-  auto key_at = [&](int j) {
+  auto key_of = [&](int j) {
     const size_t v = vec_of(j);
     const uint32_t k = weight_order(a.kv.weight[v]);
     return a.recent > 0 && (int64_t)a.kv.place[v] > since ? kProtected : k;
   };
-  if (cached)
-    for (int j = tid; j < n; j += NT) keys[j] = key_at(j);
-  auto key_of = [&](int j) { return cached ? keys[j] : key_at(j); };
   // the keep-th largest key: `prefix`, of which `need` stay
   uint32_t prefix = 0;
   int need = keep;
@@ -735,27 +920,10 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs a, int cached) {
         atomicAdd(&sh.hist[(k >> shift) & ((1u << width) - 1u)], 1u);
     }
     __syncthreads();
-    // wave 0: each lane the sum of 32 bins, the largest in lane 0; then the bins of the lane that `need` falls to
-    if (wv == 0) {
-      uint32_t sum = 0;
-      for (int i = 0; i < 32; ++i) sum += sh.hist[kBins - 1 - (lane * 32 + i)];
-      uint32_t upto = sum;
-      for (int i = 1; i < 64; i *= 2) {
-        const uint32_t o = __shfl_up(upto, i);
-        upto += lane >= i ? o : 0u;
-      }
-      const uint64_t who = __ballot(upto >= (uint32_t)need);
-      if (lane == __builtin_ctzll(who)) {                  // (n > keep >= need: one has it; need = 0: lane 0)
-        uint32_t before = upto - sum;
-        int b = kBins - 1 - lane * 32;
-        while (before + sh.hist[b] < (uint32_t)need) before += sh.hist[b--];
-        sh.prefix = prefix | ((uint32_t)b << shift);
-        sh.need = need - (int)before;
-      }
-    }
+    find_digit<kWaves>(sh.hist, sh.digits, sh.found, need);
+    prefix |= sh.found[0] << shift;
+    need = (int)sh.found[1];
     __syncthreads();
-    prefix = sh.prefix;
-    need = sh.need;
   }
   // Every wave a run of whole words of bits: how many equal the keep-th, then which stay.
   const int words = (n + 63) / 64, per = (words + kWaves - 1) / kWaves;
@@ -864,12 +1032,12 @@ hipError_t launch_marks(const MarksArgs& a, bool write, hipStream_t s) {
 }
 
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
-  const int bits = (a.max_len + 63) / 64 * 8;
-  const int cached = a.max_len <= 16384;
-  const int lds = (int)sizeof(EvictLds) + bits + (cached ? a.max_len * 4 : 0);
   const dim3 grid((unsigned)((int64_t)a.b.n_seqs * a.kv.kv_heads));
-  if (a.max_len <= 4096) hipLaunchKernelGGL(k_evict<256>, grid, dim3(256), lds, s, a, cached);
-  else hipLaunchKernelGGL(k_evict<1024>, grid, dim3(1024), lds, s, a, cached);
+  if (a.max_len <= 1024) hipLaunchKernelGGL((k_evict<256, 4>), grid, dim3(256), 0, s, a);
+  else if (a.max_len <= 4096) hipLaunchKernelGGL((k_evict<512, 8>), grid, dim3(512), 0, s, a);
+  else if (a.max_len <= kEvictShort) hipLaunchKernelGGL((k_evict<1024, 16>), grid, dim3(1024), 0, s, a);
+  else
+    hipLaunchKernelGGL(k_evict_long, grid, dim3(1024), (int)sizeof(EvictLongLds) + (a.max_len + 63) / 64 * 8, s, a);
   return hipGetLastError();
 }
 
