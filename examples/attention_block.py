@@ -4,12 +4,10 @@ Users of two domains share their domain's prompt. Per step:
 
     q, k, v = x W_q, x W_k, x W_v       salt_base_product   (8-bit weights, blocks of 128)
     q, k, v += the users' adapters       salt_apply_batch    (domain centroid + user residual)
+    q, k rotated by their positions      salt_rotate         (a user's tokens stand behind the prompt)
     k, v into the cache                  salt_kv_write       (pages, 8 bits)
     attention over prompt and history    salt_attend         (a domain's prompt is read once)
     y = attention W_o, += the adapters   salt_base_product, salt_apply
-
-This block encodes no positions. A model that rotates q and k does so with a kernel of its own between the second
-line and the third: libsalt has no such operator.
 
     python examples/attention_block.py [steps]
 
@@ -29,6 +27,7 @@ HIDDEN, HEADS, KV_HEADS, DIM = 512, 8, 2, 64
 KV = KV_HEADS * DIM
 DOMAINS, PROMPT, USERS, PAGE = 2, (200, 131), 6, 64
 RANK_C, RANK_U = 16, 2
+FREQ = 10000.0 ** (-np.arange(0, DIM, 2) / DIM)                                  # radians per position
 TABLES = [(HIDDEN, HIDDEN), (HIDDEN, KV), (HIDDEN, KV), (HIDDEN, HIDDEN)]       # q, k, v, o
 Q, K, V, O = range(4)
 
@@ -71,6 +70,7 @@ class Layer:
             self.res.append([(a[1], b[1]) for a, b in parts])
         ctx.wait_loads()
         self.plan = ctx.plan()
+        self.rotation = ctx.rotation(HEADS, KV_HEADS, DIM, FREQ)
         # one layer's cache; every user and every domain's prompt has pages of its own
         self.kv = ctx.kv_cache(1, HEADS, KV_HEADS, DIM, PAGE, 64)
         self.step_seqs = self.kv.seqs(USERS + DOMAINS, most_tokens, 64)
@@ -82,10 +82,13 @@ class Layer:
 
     def run(self, x_bits, domain_of, user_of, q_len, length, pages, domain=None):
         """One step of the block for a batch of sequences; returns the output rows."""
+        # positions of the new tokens: behind the domain's prompt
+        base = [0 if domain is None else PROMPT[domain[i]] for i in range(len(q_len))]
+        pos = np.concatenate([b + n - q + np.arange(q) for b, n, q in zip(base, length, q_len)]).astype(np.int32)
         hip, ctx, s, T = self.hip, self.ctx, self.stream.h, len(x_bits)
         x = hip.DeviceArray.from_host(x_bits)
         y = [hip.DeviceArray((T, n_out), np.uint16) for _, n_out in TABLES]
-        att = hip.DeviceArray((T, HIDDEN), np.uint16)
+        att, at = hip.DeviceArray((T, HIDDEN), np.uint16), hip.DeviceArray.from_host(pos)
         self.plan.set_maps(domain_of, user_of, None, s)
         self.plan.build(s)
         off = np.concatenate([[0], np.cumsum([len(p) for p in pages])])
@@ -95,13 +98,14 @@ class Layer:
         # q, k and v read one x: one product, one apply
         ctx.base_product([Q, K, V], T, x.ptr, [y[t].ptr for t in (Q, K, V)], s)
         ctx.apply_batch([Q, K, V], self.plan, [x.ptr] * 3, [y[t].ptr for t in (Q, K, V)], s)
+        ctx.rotate(self.rotation, T, at.ptr, y[Q].ptr, y[Q].ptr, y[K].ptr, y[K].ptr, s)
         self.step_seqs.write(0, y[K].ptr, y[V].ptr, s)
         self.step_seqs.attend(0, y[Q].ptr, att.ptr, DIM ** -0.5, s)
         ctx.base_product([O], T, att.ptr, [y[O].ptr], s)
         ctx.apply(O, self.plan, att.ptr, y[O].ptr, s)
         self.stream.synchronize()
         out = decode(y[O].to_host())
-        for d in [x, att, *y]:
+        for d in [x, att, at, *y]:
             d.free()
         return out
 
@@ -115,11 +119,21 @@ class Layer:
             y = y + (x @ a.T) @ r
         return y
 
+    @staticmethod
+    def rotate(x, pos):
+        """Heads of x [rows][heads * DIM]: values i and i + DIM / 2 turn by pos * FREQ[i]."""
+        v = x.reshape(len(x), -1, 2, DIM // 2)
+        t = (pos[:, None] * FREQ)[:, None, :]
+        a, b = v[:, :, 0], v[:, :, 1]
+        return np.stack([a * np.cos(t) - b * np.sin(t), b * np.cos(t) + a * np.sin(t)], 2).reshape(x.shape)
+
     def reference(self, x, holder, prompt, d, u):
         """x: a sequence's new rows; holder: where its history is kept; prompt: None or a domain."""
         q, k, v = (self.project(t, x, d, u) for t in (Q, K, V))
         hk, hv = self.history.get(holder, (np.zeros((0, KV)),) * 2)
         before = len(hk)
+        pos = (PROMPT[prompt] if prompt is not None else 0) + before + np.arange(len(x))
+        q, k = self.rotate(q, pos), self.rotate(k, pos)
         hk, hv = np.concatenate([hk, k]), np.concatenate([hv, v])
         self.history[holder] = hk, hv
         pk, pv = self.history[("prompt", prompt)] if prompt is not None else (np.zeros((0, KV)),) * 2

@@ -539,8 +539,8 @@ SALT_API salt_status salt_rotate(salt_ctx* ctx, const salt_rotation* rot, int32_
  * sequences to a budget scores each step and evicts the tokens of least weight:
  *     salt_kv_write, salt_attend, salt_kv_score, [salt_kv_evict]   for every layer of a step.
  *
- * salt_kv_track allocates the marks of every layer and page and clears them (blocking, once; a
- * second call does nothing).  Errors: SALT_ERR_INVALID_ARG, SALT_ERR_OUT_OF_MEMORY. */
+ * salt_kv_track allocates the marks of every layer and page and clears them (blocking, once, before work of the
+ * cache is recorded into a graph; a second call does nothing).  Errors: SALT_ERR_INVALID_ARG, SALT_ERR_OUT_OF_MEMORY. */
 SALT_API salt_status salt_kv_track(salt_ctx* ctx, salt_kv* kv);
 /* After salt_kv_write of the step, with the q and scale of salt_attend: to token j of a sequence, for each
  * kv head, add
@@ -550,7 +550,8 @@ SALT_API salt_status salt_kv_track(salt_ctx* ctx, salt_kv* kv);
  * all of them for window = 0.  The step's own new tokens start at w_j, whatever their marks
  * held, and take the position pos[t] (device, [T]; NULL: their place in the sequence); so each step
  * is scored once.  A prefix has no marks.  A row with a logit of NaN or +inf, or none above -inf, adds NaN
- * to all that it sees.  fp32 sums, reproducible bit for bit; q and keys as in salt_attend, the weights unrounded. */
+ * to all that it sees.  fp32 sums, reproducible bit for bit; q and keys as in salt_attend, the weights unrounded.  Rows
+ * of q are at most 2^24 elements apart (SALT_ERR_OUT_OF_RANGE). */
 SALT_API salt_status salt_kv_score(salt_ctx* ctx, salt_seqs* seqs, int32_t layer, const void* q, int64_t ldq,
                                    const int32_t* pos, float scale, int32_t window, void* stream);
 /* For every sequence of the batch with n = len > keep own tokens, each kv head by itself, keep `keep` tokens:

@@ -366,3 +366,137 @@ def test_copies(dim, kv_heads, page, fmt, layers, tracked):
                 assert np.array_equal(a, o)
     finally:
         b.close()
+
+
+# ---- layouts and values beyond the kinds above --------------------------------------------------------
+@pytest.mark.parametrize("group", [1, 2, 3, 5, 6, 7, 8, 12, 16, 17, 24, 33, 64])
+@pytest.mark.parametrize("dtype,dim", [("bf16", 64), ("f32", 64), ("bf16", 128)])
+def test_score_groups_of_heads(group, dtype, dim):
+    """Sequences of many rows for every way that a group's heads fill a tile of 16 rows; and few rows beside them."""
+    print(f"\n[gpu case] score group={group} {dtype} dim={dim}", flush=True)
+    b = Tracked([200 // group + 3, 1, 133 // group + 1], [200 // group + 70, 65, 133 // group + 1], heads=2 * group, kv_heads=2,
+                dim=dim, page=64, dtype=dtype, prefix=[40], domain=[0, -1, -1]).open()
+    try:
+        b.fill()
+        b.set()
+        b.check_score()
+        b.check_score(window=150 // group + 1, ldq=2 * group * dim + 8)
+    finally:
+        b.close()
+
+
+@pytest.mark.parametrize("page", [16, 32, 256])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_score_of_many_rows_over_pages(page, fmt):
+    """Units that end inside a page, and pages that end inside a unit."""
+    print(f"\n[gpu case] score pages of {page} {fmt}", flush=True)
+    b = Tracked([90, 130, 64], [155, 130, 320], heads=8, kv_heads=2, dim=64, page=page, fmt=fmt, dtype="bf16", layers=2).open()
+    try:
+        b.fill(0)
+        b.set()
+        b.check_score()
+    finally:
+        b.close()
+
+
+@pytest.mark.parametrize("kind", ["decode", "drafts", "prompts", "a long prompt"])
+@pytest.mark.parametrize("what", ["k", "v"])
+def test_keys_that_are_not_finite(kind, what):
+    """A key (or value) with a NaN: the rows that see it add NaN to all they see, and to nothing else."""
+    print(f"\n[gpu case] score NaN in {what}, {kind}", flush=True)
+    b = Tracked(heads=4, kv_heads=2, dim=64, page=16, **KINDS[kind]).open()
+    try:
+        b.fill()
+        b.set()
+        b.put()
+        b.score()
+        clean, _ = b.get()
+        s = int(np.argmax(b.q_len))
+        j = int(b.length[s]) - int(b.q_len[s]) // 2 - 1             # seen by the sequence's last rows alone
+        arr = [a.copy() for a in (b.k if what == "k" else b.v)]
+        arr[s][j, 1, 3] = np.nan
+        b.fill(**{what: arr})
+        b.put()
+        b.score()
+        got, _ = b.get()
+        row0 = int(np.sum(b.length[:s]))
+        hit = np.zeros(clean.shape, bool)
+        hit[row0: row0 + int(b.length[s]), 1] = True
+        assert np.isnan(got[hit]).all() and np.array_equal(got[~hit], clean[~hit])
+    finally:
+        b.close()
+
+
+@pytest.mark.parametrize("n", [255, 256, 257, 511, 1023, 1024, 1025, 2047, 4095, 16383])
+@pytest.mark.parametrize("drop", [1, 3])
+def test_a_few_over_the_budget(n, drop):
+    """The step of a bounded server, at sizes around a block's rows of tokens; equal weights among them."""
+    print(f"\n[gpu case] evict {drop} of {n}", flush=True)
+    b = Tracked([0], [n], heads=2, kv_heads=2, dim=64, page=64, dtype="bf16").open()
+    b.weight = np.round(b.weight, 1).astype(np.float32)
+    try:
+        b.fill()
+        b.set()
+        _evict(b, n - drop, min(20, n - drop))
+    finally:
+        b.close()
+
+
+def test_two_streams():
+    """Scores and evictions of one cache from two streams and two objects in turn: ordered by the library."""
+    print("\n[gpu case] marks from two streams", flush=True)
+    hip = hipmod()
+    b = Tracked([1, 40], [600, 90], heads=4, kv_heads=2, dim=64, page=16).open()
+    try:
+        b.fill()
+        b.set()
+        b.put()
+        b.score()
+        b.seqs.evict(0, 50, 5, b.stream.h)
+        want = b.get()
+        other, mine = b.kv.seqs(2, 41, 60), b.stream
+        second = hip.Stream()
+        b.set(other, second)
+        for _ in range(3):
+            b.fill()
+            d = [to_dev(b.weight), to_dev(b.place)]
+            q = to_dev(store(b.q, b.dtype))
+            out = [to_dev(np.zeros((690, 2), t)) for t in (np.float32, np.int32)]
+            b.seqs.write_marks(0, d[0].ptr, d[1].ptr, mine.h)
+            other.score(0, q.ptr, 0, b.scale, 0, second.h)
+            b.seqs.evict(0, 50, 5, mine.h)
+            other.read_marks(0, out[0].ptr, out[1].ptr, second.h)
+            second.synchronize()
+            mine.synchronize()
+            for o, w in zip(out, want):
+                assert np.array_equal(o.to_host(), w)
+        b.stream = mine
+        other.close()
+        second.destroy()
+    finally:
+        b.close()
+
+
+def test_a_pool_past_4_gib():
+    """Pages whose codes lie past 4 GiB: marks, scores, an eviction and copies there."""
+    print("\n[gpu case] pool past 4 GiB", flush=True)
+    n_pages = (5 << 30) // (256 * 8 * 256) + 4                     # of k alone
+    b = Tracked([1, 70], [300, 70], heads=8, kv_heads=8, dim=256, page=256, dtype="bf16", spare=0)
+    shift = n_pages - b.n_pages
+    b.pages = (b.pages + shift).astype(np.int32)
+    b.open(n_pages)
+    try:
+        b.fill()
+        b.set()
+        b.check_score()
+        b.fill()
+        _evict(b, 64, 8)
+        b.fill()
+        b.put()
+        b.kv.copy(b.pages, np.arange(len(b.pages)), None, b.stream.h)
+        low = b.kv.seqs(2, 71, 8)
+        low.set(b.q_len, b.length, b.page_off, np.arange(len(b.pages)), stream=b.stream.h)
+        for a, w in zip(b.get(seqs=low), (b.weight, b.place)):
+            assert np.array_equal(a, w)
+    finally:
+        b.close()

@@ -155,3 +155,44 @@ def test_one_operand_alone():
             assert np.array_equal(o.to_host(), w)
     finally:
         ctx.close()
+
+
+def test_refusals_leave_the_values():
+    print("\n[gpu case] rotate refusals", flush=True)
+    hip = hipmod()
+    ctx = salt.Context("bf16", [(64, 64)], 0, 0, 1, 0, 1)
+    try:
+        x, pos = to_dev(np.full((2, 192), 5, np.uint16)), to_dev(np.arange(2, dtype=np.int32))
+        ok = ctx.rotation(2, 1, 64, _freq(64))
+        p = x.ptr
+        for rot, args in ((ctx.rotation(2, 1, 60, _freq(56)), (2, pos.ptr, p, p, p, p)),
+                          (ctx.rotation(2, 1, 64, _freq(72)), (2, pos.ptr, p, p, p, p)),
+                          (ctx.rotation(2, 1, 64, np.full(32, np.nan)), (2, pos.ptr, p, p, p, p)),
+                          (ok, (2, 0, p, p, p, p)), (ok, (2, pos.ptr, p + 2, p, p, p)), (ok, (2, pos.ptr, p, 0, p, p))):
+            assert ctx.rotate_status(rot, *args) == salt.ERR_INVALID_ARG
+        assert ctx.rotate_status(ok, -1, pos.ptr, p, p, p, p) == salt.ERR_OUT_OF_RANGE
+        assert ctx.rotate_status(ok, 2, pos.ptr, p, p, p, p, ldq=192, ldqo=200) == salt.ERR_INVALID_ARG
+        hip.synchronize()
+        assert np.all(x.to_host() == 5)
+    finally:
+        ctx.close()
+
+
+def test_q_and_k_of_one_buffer():
+    """q and k as columns of one buffer of rows (a joint projection's output), in place; v beside them stays."""
+    print("\n[gpu case] rotate in one buffer", flush=True)
+    c = Case(9, 4, 2, 64, 64, "bf16", False, True, np.arange(9) * 100)
+    want = c.run()
+    hip, ctx = hipmod(), salt.Context("bf16", [(64, 64)], 0, 0, 1, 0, 1)
+    try:
+        buf = np.full((9, 512), 77, np.uint16)
+        buf[:, :256], buf[:, 256:384] = store(c.q, "bf16").reshape(9, -1), store(c.k, "bf16").reshape(9, -1)
+        d, pos, n = to_dev(buf), to_dev(c.pos), [to_dev(store(x, "bf16")) for x in c.norms]
+        rot = ctx.rotation(4, 2, 64, c.freq, False, n[0].ptr, n[1].ptr, c.eps)
+        ctx.rotate(rot, 9, pos.ptr, d.ptr, d.ptr, d.ptr + 512, d.ptr + 512, 0, 512, 512, 512, 512)
+        hip.synchronize()
+        got = d.to_host()
+        assert np.array_equal(got[:, :256], store(want[0], "bf16").reshape(9, -1))
+        assert np.array_equal(got[:, 256:384], store(want[1], "bf16").reshape(9, -1)) and np.all(got[:, 384:] == 77)
+    finally:
+        ctx.close()
