@@ -49,6 +49,13 @@ __device__ __forceinline__ void load_query(const E* q, int g, bool used, uint4 (
   }
 }
 
+// What the wave's lanes wrote to LDS before is there for all of them after.  (LDS keeps a wave's order: the compiler has to.)
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Rows of kBytes that a wave stages in LDS of its own.  An operand load straight from memory gives neighbouring lanes
 // neighbouring rows: 64 cache lines to an instruction, which the address unit takes a cycle each for (rows of q read so:
 // k_score_many 330 us on the prompts above, 107 with its loads left out).  From here the wave reads memory in order,
@@ -231,9 +238,10 @@ __device__ __forceinline__ void stat_item(const ScoreArgs& sa, const AttItem& it
       for (int e = 0; e < 8; ++e) l[t] += __builtin_amdgcn_exp2f(z[t][e]);
   };
   auto put = [&](const Keys32<D>& x) {
+    wave_order();                                          // (the keys before have been read)
 #pragma unroll
     for (int u = 0; u < 2; ++u) stage_keys<D>(stage + u * 16 * D, lane, x.c[u]);
-    __builtin_amdgcn_wave_barrier();
+    wave_order();
   };
   Keys32<D> y;
   for (; st < st1; st += 2 * WK) {
@@ -411,9 +419,9 @@ __device__ __forceinline__ void convert_unit(const UnitCodes<D>& u, float c, int
     x.ks[t][0] = u.s[t].x * c; x.ks[t][1] = u.s[t].y * c; x.ks[t][2] = u.s[t].z * c; x.ks[t][3] = u.s[t].w * c;
     uint32_t w[D / 16];
     stage_keys<D>(stage + (t & 1) * 16 * D, lane, u.c[t]);   // (LDS keeps a wave's order)
-    __builtin_amdgcn_wave_barrier();
+    wave_order();
     read_keys<D>(stage + (t & 1) * 16 * D, lane, w);
-    __builtin_amdgcn_wave_barrier();
+    wave_order();
     keys_bf16<D, FMT>(w, x.k[t]);
   }
 }
@@ -593,7 +601,7 @@ __global__ void __launch_bounds__(256, sizeof(E) * D <= 256 ? 2 : 1) k_score_man
 #pragma unroll
     for (int k = 0; k < S::kChunks / 4; ++k)
       *reinterpret_cast<u32x4*>(stage + S::at(S::row(k, lane), S::chunk(k, lane))) = c[k];
-    __builtin_amdgcn_wave_barrier();
+    wave_order();
   };
   auto take = [&](uint4 (&q)[terms<E>()][D / 32]) {
 #pragma unroll
@@ -614,7 +622,7 @@ __global__ void __launch_bounds__(256, sizeof(E) * D <= 256 ? 2 : 1) k_score_man
         for (int n = 0; n < terms<E>(); ++n) q[n][ks] = t[n];
       }
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_order();
   };
   uint4 q[terms<E>()][D / 32];
   if (full < tiles && wave == (full & 3)) {                // the tile that is short of tokens
