@@ -538,6 +538,10 @@ SALT_API salt_status salt_rotate(salt_ctx* ctx, const salt_rotation* rot, int32_
  * token has gathered from the queries so far (fp32), and its position.  A server that holds its
  * sequences to a budget scores each step and evicts the tokens of least weight:
  *     salt_kv_write, salt_attend, salt_kv_score, [salt_kv_evict]   for every layer of a step.
+ * salt_kv_write starts the marks of the tokens that it writes: weight 0, and for a position the place in the
+ * sequence.  So a page says nothing of a sequence that had it before, and a step need not be scored (the chunks of a
+ * prompt but the last, say).  Where salt_kv_write_marks gave the batch's marks of the layer first, they stay.
+ * (Behind an eviction a place is no position any more: there a step is scored with pos, or given its marks.)
  *
  * salt_kv_track allocates the marks of every layer and page and clears them (blocking, once, before work of the
  * cache is recorded into a graph; a second call does nothing).  Errors: SALT_ERR_INVALID_ARG, SALT_ERR_OUT_OF_MEMORY. */
@@ -548,8 +552,8 @@ SALT_API salt_status salt_kv_track(salt_ctx* ctx, salt_kv* kv);
  * over the sequence's counted new tokens t that see j and the query heads h of the kv head; i runs over all
  * keys of salt_attend, a domain's prefix too.  Counted are the last `window` new tokens of each sequence,
  * all of them for window = 0.  The step's own new tokens start at w_j, whatever their marks
- * held, and take the position pos[t] (device, [T]; NULL: their place in the sequence); so each step
- * is scored once.  A prefix has no marks.  A row with a logit of NaN or +inf, or none above -inf, adds NaN
+ * held, and take the position pos[t] (device, [T]; NULL: their place in the sequence); so a step
+ * is scored once at most.  A prefix has no marks.  A row with a logit of NaN or +inf, or none above -inf, adds NaN
  * to all that it sees.  fp32 sums, reproducible bit for bit; q and keys as in salt_attend, the weights unrounded.  Rows
  * of q are at most 2^24 elements apart (SALT_ERR_OUT_OF_RANGE). */
 SALT_API salt_status salt_kv_score(salt_ctx* ctx, salt_seqs* seqs, int32_t layer, const void* q, int64_t ldq,

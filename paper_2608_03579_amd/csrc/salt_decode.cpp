@@ -78,6 +78,7 @@ salt_status marks_copy(salt_ctx* ctx, salt_seqs* q, int32_t layer, float* weight
   a.weight = weight;
   a.place = place;
   SERVE_HIP(ctx, salt::launch_marks(a, write, s));
+  if (write) q->given[(size_t)layer] = 1;
   return SALT_OK;
 }
 

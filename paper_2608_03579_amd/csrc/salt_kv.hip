@@ -149,6 +149,10 @@ __global__ void __launch_bounds__(256) k_kv_write(KvWriteArgs a) {
   if (l == 0) {
     a.kv.ks[at] = ks;
     a.kv.vs[at] = vs;
+    if (a.place) {                            // (the page may hold another sequence's marks)
+      a.kv.weight[at] = 0.f;
+      a.kv.place[at] = a.place[t];
+    }
   }
 }
 

@@ -105,9 +105,10 @@ struct salt_seqs {
   int n_seqs = 0, max_len = 0;        // the longest sequence that it has
   bool recorded = false;              // a graph holds its launches: grid sizes and places in `dev`
   size_t at_page = 0, at_row = 0, at_count = 0, at_slot = 0, at_order = 0, at_item = 0, at_join = 0;
-  size_t at_unit = 0, at_rec = 0, at_back = 0, at_joined = 0;
+  size_t at_unit = 0, at_rec = 0, at_back = 0, at_joined = 0, at_place = 0;
   int n_units = 0, min_q = 0, max_q = 0;   // units of own keys; new tokens of a sequence that has any
   int n_kind[4] = {0, 0, 0, 0}, n_joins = 0;
+  std::vector<uint8_t> given;         // per layer: salt_kv_write_marks gave the batch's marks
 };
 
 namespace salt {

@@ -387,9 +387,9 @@ salt_status salt_seqs_create(salt_ctx* ctx, salt_kv* kv, int32_t max_seqs, int32
   q->max_pages = max_pages;
   const size_t T = (size_t)max_tokens;
   const size_t items = (size_t)salt::attend_max_items(max_tokens, kv->cfg.n_heads);
-  // (each of the ten arrays behind the first starts at a multiple of 16 words)
-  q->words = 3 * (size_t)max_pages + (size_t)salt::most_units(max_pages, kv->cfg.page_tokens) + 5 * T +
-             (sizeof(salt::SeqRec) / 4) * (size_t)max_seqs + 10 * 16 + items * (sizeof(salt::AttItem) / 4) + T * (sizeof(salt::AttJoin) / 4);
+  // (each of the eleven arrays behind the first starts at a multiple of 16 words)
+  q->words = 3 * (size_t)max_pages + (size_t)salt::most_units(max_pages, kv->cfg.page_tokens) + 6 * T +
+             (sizeof(salt::SeqRec) / 4) * (size_t)max_seqs + 11 * 16 + items * (sizeof(salt::AttItem) / 4) + T * (sizeof(salt::AttJoin) / 4);
   q->part_rows = (int64_t)(2 * T * (size_t)kv->cfg.n_heads) + salt::kExtraRows;
   if (q->part_rows > INT32_MAX) {
     free_seqs(q);
@@ -406,6 +406,7 @@ salt_status salt_seqs_create(salt_ctx* ctx, salt_kv* kv, int32_t max_seqs, int32
     return ctx_fail(ctx, SALT_ERR_OUT_OF_MEMORY, "buffers for %d sequences of %d new tokens", max_seqs, max_tokens);
   }
   try {
+    q->given.assign((size_t)kv->cfg.n_layers, 0);
     kv->seqs.push_back(q);
   } catch (const std::bad_alloc&) {
     free_seqs(q);
@@ -507,7 +508,8 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
     const size_t at_unit = at_join + words(w.joins.size() * (sizeof(salt::AttJoin) / 4));
     const size_t at_rec = at_unit + words((size_t)n_units);
     const size_t at_back = at_rec + words((size_t)n * (sizeof(salt::SeqRec) / 4));
-    const size_t at_joined = at_back + words((size_t)T), total = at_joined + (size_t)T;
+    const size_t at_joined = at_back + words((size_t)T), at_place = at_joined + words((size_t)T);
+    const size_t total = at_place + (size_t)T;
     if (total > q->words || w.rows > q->part_rows)
       return ctx_fail(ctx, SALT_ERR_BAD_STATE, "%zu words and %lld partial rows exceed the sequences' %zu and %lld",
                       total, (long long)w.rows, q->words, (long long)q->part_rows);
@@ -542,6 +544,7 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
       for (int j = 0; j < b->q_len[i]; ++j, ++t) {
         const int pos = first + j;
         d[at_back + t] = b->q_len[i] - 1 - j;
+        d[at_place + t] = pos;
         d[at_slot + t] = pos < 0 ? -1 : pages[pos / pt] * pt + pos % pt;
         if (pos >= 0 && (pos % pt == 0 || pos == std::max(first, 0))) {
           uint32_t& st_ = kv->stamp[(size_t)pages[pos / pt]];
@@ -590,6 +593,7 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
     q->at_join = at_join;
     q->at_unit = at_unit;
     q->at_joined = at_joined;
+    q->at_place = at_place;
     q->n_units = unit;
     q->min_q = min_q;
     q->max_q = max_q;
@@ -597,6 +601,7 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
     q->at_back = at_back;
     std::copy(w.n_kind, w.n_kind + 4, q->n_kind);
     q->n_joins = (int)w.joins.size();
+    std::fill(q->given.begin(), q->given.end(), (uint8_t)0);
   } catch (const std::bad_alloc&) {
     return ctx_fail(ctx, SALT_ERR_OUT_OF_MEMORY, "cutting the batch");
   }
@@ -624,6 +629,7 @@ salt_status salt_kv_write(salt_ctx* ctx, salt_seqs* q, int32_t layer, const void
   a.ldk = ldk;
   a.ldv = ldv;
   a.slot = q->dev + q->at_slot;
+  if (kv->marks && !q->given[(size_t)layer]) a.place = q->dev + q->at_place;
   a.T = q->T;
   SERVE_HIP(ctx, salt::launch_kv_write(a, cv.bf16, s));
   return SALT_OK;

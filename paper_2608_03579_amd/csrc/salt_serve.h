@@ -91,6 +91,7 @@ struct KvWriteArgs {
   const void *k, *v;        // [T][ld], kv head h at h * dim
   int64_t ldk, ldv;         // elements
   const int32_t* slot;      // [T]: page * page tokens + place, or -1
+  const int32_t* place;     // [T]: place in the sequence, where the tokens' marks start; null: marks stay as they are
   int32_t T;
 };
 struct KvReadArgs {
