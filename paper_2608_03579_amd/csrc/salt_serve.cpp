@@ -564,7 +564,7 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
       }
       row += len;
     }
-    std::memcpy(d + at_order, w.order.data(), w.order.size() * 4);
+    if (!w.order.empty()) std::memcpy(d + at_order, w.order.data(), w.order.size() * 4);
     if (!w.items.empty()) std::memcpy(d + at_item, w.items.data(), w.items.size() * sizeof(salt::AttItem));
     std::fill(d + at_joined, d + at_joined + T, -1);
     for (size_t j = 0; j < w.joins.size(); ++j) d[at_joined + w.joins[j].tok] = (int32_t)j;

@@ -109,6 +109,7 @@ static int written() {
   need(w.write(0) == SALT_OK && g_write.place, "the other layer");
   need(w.set({1}, {-1}, {}) != SALT_OK && w.write(1) == SALT_OK && !g_write.place, "the batch that stays behind a refused one");
   need(w.set({1}, {41}, {0, 1, 2}) == SALT_OK && w.write(1) == SALT_OK && g_write.place && g_write.place[0] == 40, "the next batch");
+  need(w.set({0}, {7}, {3}) == SALT_OK && w.write(0) == SALT_OK, "a batch without new tokens");
   World plain(false);
   need(plain.set({2}, {40}, {0, 1, 2}) == SALT_OK && plain.write(0) == SALT_OK && !g_write.place, "an untracked cache");
   need(salt_kv_track(plain.c, plain.kv) == SALT_OK && plain.write(0) == SALT_OK && g_write.place && g_write.place[1] == 39,
