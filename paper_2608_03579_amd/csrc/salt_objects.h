@@ -78,8 +78,7 @@ struct salt_kv {
   size_t codes = 0, scales = 0;       // bytes of one layer's k (or v) codes, and scales
   std::vector<salt_seqs*> seqs;
   char* marks = nullptr;              // gathered weights and positions (salt_kv_track), layer after layer
-  std::vector<uint32_t> stamp;        // per page: the salt_seqs_set that last saw it written
-  std::vector<uint32_t> held;         // and the one that last saw tokens in it
+  std::vector<uint32_t> stamp;        // per page: the last count of `stamps` that met it
   uint32_t stamps = 0;
   salt::StreamOrder order;                  // writes and reads of the pool
 };
@@ -101,17 +100,28 @@ struct salt_seqs {
   int n_refs = 0, n_own_refs = 0;
   int64_t own_tokens = 0;
   bool clash = false;                 // two of its tokens' pages are one page
-  bool shared = false;                // a page holds own tokens twice, or beside a prefix
+  int shared = -1;                    // a page holds own tokens twice, or beside a prefix (-1: not looked at yet)
   int n_seqs = 0, max_len = 0;        // the longest sequence that it has
   bool recorded = false;              // a graph holds its launches: grid sizes and places in `dev`
   size_t at_page = 0, at_row = 0, at_count = 0, at_slot = 0, at_order = 0, at_item = 0, at_join = 0;
   size_t at_unit = 0, at_rec = 0, at_back = 0, at_joined = 0, at_place = 0;
+  size_t at_prefix = 0;               // in `staging` alone: first page reference and pages in use of each prefix
+  int n_domains = 0;
   int n_units = 0, min_q = 0, max_q = 0;   // units of own keys; new tokens of a sequence that has any
   int n_kind[4] = {0, 0, 0, 0}, n_joins = 0;
   std::vector<uint8_t> given;         // per layer: salt_kv_write_marks gave the batch's marks
 };
 
 namespace salt {
+
+// A number that no page is stamped with.
+inline uint32_t next_stamp(salt_kv* kv) {
+  if (++kv->stamps == 0) {
+    std::fill(kv->stamp.begin(), kv->stamp.end(), 0u);
+    kv->stamps = 1;
+  }
+  return kv->stamps;
+}
 
 // Whether `kv` is a live cache of `ctx` (asked before anything of it is read).
 inline salt_status kv_of(salt_ctx* ctx, const salt_kv* kv) {

@@ -333,7 +333,6 @@ salt_status salt_kv_create(salt_ctx* ctx, const salt_kv_config* cfg, salt_kv** o
   const size_t bytes = salt_kv_bytes(cfg);
   try {
     kv->stamp.assign((size_t)cfg->n_pages, 0);
-    kv->held.assign((size_t)cfg->n_pages, 0);
   } catch (const std::bad_alloc&) {
     free_kv(kv);
     return ctx_fail(ctx, SALT_ERR_OUT_OF_MEMORY, "cache");
@@ -387,9 +386,9 @@ salt_status salt_seqs_create(salt_ctx* ctx, salt_kv* kv, int32_t max_seqs, int32
   q->max_pages = max_pages;
   const size_t T = (size_t)max_tokens;
   const size_t items = (size_t)salt::attend_max_items(max_tokens, kv->cfg.n_heads);
-  // (each of the eleven arrays behind the first starts at a multiple of 16 words)
+  // (each of the eleven arrays behind the first starts at a multiple of 16 words; the last one's two words a domain)
   q->words = 3 * (size_t)max_pages + (size_t)salt::most_units(max_pages, kv->cfg.page_tokens) + 6 * T +
-             (sizeof(salt::SeqRec) / 4) * (size_t)max_seqs + 11 * 16 + items * (sizeof(salt::AttItem) / 4) + T * (sizeof(salt::AttJoin) / 4);
+             (sizeof(salt::SeqRec) / 4 + 2) * (size_t)max_seqs + 11 * 16 + items * (sizeof(salt::AttItem) / 4) + T * (sizeof(salt::AttJoin) / 4);
   q->part_rows = (int64_t)(2 * T * (size_t)kv->cfg.n_heads) + salt::kExtraRows;
   if (q->part_rows > INT32_MAX) {
     free_seqs(q);
@@ -441,7 +440,7 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
   if ((n > 0 && (!b->q_len || !b->len || !b->page_off)) || (nd > 0 && (!b->prefix_len || !b->prefix_off)))
     return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "null array");
   salt_kv* kv = q->kv;
-  const int pt = kv->cfg.page_tokens;
+  const int pt = kv->cfg.page_tokens, lp = kv->log2_page;
   // page references of one kind of holder: offsets from 0 on, enough pages for the tokens
   auto refs = [&](const char* what, int count, const int32_t* off, const int32_t* len, const int32_t* pages) {
     if (count > 0 && off[0] != 0) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "%s: page offsets start at 0", what);
@@ -510,9 +509,10 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
     const size_t at_back = at_rec + words((size_t)n * (sizeof(salt::SeqRec) / 4));
     const size_t at_joined = at_back + words((size_t)T), at_place = at_joined + words((size_t)T);
     const size_t total = at_place + (size_t)T;
-    if (total > q->words || w.rows > q->part_rows)
+    const size_t at_prefix = total, all = at_prefix + 2 * (size_t)nd;
+    if (all > q->words || w.rows > q->part_rows)
       return ctx_fail(ctx, SALT_ERR_BAD_STATE, "%zu words and %lld partial rows exceed the sequences' %zu and %lld",
-                      total, (long long)w.rows, q->words, (long long)q->part_rows);
+                      all, (long long)w.rows, q->words, (long long)q->part_rows);
     const int stage = q->stage ^ 1;
     if (q->pending[stage]) {
       SERVE_HIP(ctx, hipEventSynchronize(q->staged[stage]));
@@ -522,15 +522,12 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
     if (pre_refs) std::memcpy(d + at_page, b->prefix_pages, (size_t)pre_refs * 4);
     if (own_refs) std::memcpy(d + at_page + pre_refs, b->pages, (size_t)own_refs * 4);
     // two tokens of the batch written into one page from two sequences would race
-    bool clash = false, shared = false;
-    if (++kv->stamps == 0) {
-      std::fill(kv->stamp.begin(), kv->stamp.end(), 0u);
-      std::fill(kv->held.begin(), kv->held.end(), 0u);
-      kv->stamps = 1;
+    bool clash = false;
+    const uint32_t now = salt::next_stamp(kv);
+    for (int i = 0; i < nd; ++i) {
+      d[at_prefix + 2 * i] = b->prefix_off[i];
+      d[at_prefix + 2 * i + 1] = ceil_div(b->prefix_len[i], pt);
     }
-    for (int i = 0; i < nd; ++i)
-      for (int k = 0; k < ceil_div(b->prefix_len[i], pt); ++k)
-        kv->held[(size_t)b->prefix_pages[b->prefix_off[i] + k]] = kv->stamps;
     int t = 0, row = 0, max_len = 0, unit = 0, min_q = 0, max_q = 0;
     salt::SeqRec* rec = reinterpret_cast<salt::SeqRec*>(d + at_rec);
     for (int i = 0; i < n; ++i) {
@@ -545,22 +542,17 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
         const int pos = first + j;
         d[at_back + t] = b->q_len[i] - 1 - j;
         d[at_place + t] = pos;
-        d[at_slot + t] = pos < 0 ? -1 : pages[pos / pt] * pt + pos % pt;
-        if (pos >= 0 && (pos % pt == 0 || pos == std::max(first, 0))) {
-          uint32_t& st_ = kv->stamp[(size_t)pages[pos / pt]];
-          clash |= st_ == kv->stamps;
-          st_ = kv->stamps;
+        d[at_slot + t] = pos < 0 ? -1 : (pages[pos >> lp] << lp) + (pos & (pt - 1));
+        if (pos >= 0 && ((pos & (pt - 1)) == 0 || pos == std::max(first, 0))) {
+          uint32_t& st_ = kv->stamp[(size_t)pages[pos >> lp]];
+          clash |= st_ == now;
+          st_ = now;
         }
       }
-      for (int r = b->page_off[i]; r < b->page_off[i + 1]; ++r) {
-        const int k = r - b->page_off[i];
-        d[at_row + r] = salt::page_row(row, len, pt, k);
-        d[at_count + r] = salt::page_count(len, pt, k);
-        if (d[at_count + r] > 0) {
-          uint32_t& held = kv->held[(size_t)b->pages[r]];
-          shared |= held == kv->stamps;
-          held = kv->stamps;
-        }
+      const int ref0 = b->page_off[i], refs = b->page_off[i + 1] - ref0;
+      for (int k = 0; k < refs; ++k) {
+        d[at_row + ref0 + k] = salt::page_row(row, len, pt, k);
+        d[at_count + ref0 + k] = salt::page_count(len, pt, k);
       }
       row += len;
     }
@@ -581,7 +573,9 @@ salt_status salt_seqs_set(salt_ctx* ctx, salt_seqs* q, const salt_seq_batch* b, 
     q->n_own_refs = own_refs;
     q->own_tokens = own;
     q->clash = clash;
-    q->shared = shared;
+    q->shared = -1;
+    q->at_prefix = at_prefix;
+    q->n_domains = nd;
     q->n_seqs = n;
     q->max_len = max_len;
     q->at_page = at_page;

@@ -2,6 +2,8 @@
 // context; the launches note their arguments and do nothing.  argv[1]:
 //   written   salt_kv_write starts the marks of the tokens that it writes, where the cache is tracked and the batch's
 //             marks of the layer were not given before.
+//   shared    a batch with a page of two sequences, or of a sequence and a domain, is refused by the calls that change
+//             marks; its pages are looked at when such a call comes, once for a batch, and not by salt_seqs_set.
 // Prints the first failure and exits 1, else "ok".
 #include <hip/hip_runtime.h>
 
@@ -118,7 +120,81 @@ static int written() {
   return 0;
 }
 
+static uint32_t g_seed = 1;
+static int draw(int n) { return (int)((g_seed = g_seed * 1664525u + 1013904223u) >> 8) % n; }
+
+static int shared() {
+  int refused = 0;
+  for (int round = 0; round < 400; ++round) {
+    const int pages = 8 + draw(56);
+    World w(round % 2 == 0, pages);
+    for (int batch = 0; batch < 4; ++batch) {
+      // holders with tables over few pages, some with references behind their last token
+      std::vector<int32_t> q_len, len, tab, off{0}, pre, pre_tab, pre_off{0};
+      auto holder = [&](std::vector<int32_t>& l, std::vector<int32_t>& t, std::vector<int32_t>& o, int most) {
+        const int refs = draw(most + 1);
+        l.push_back(refs ? draw(refs * 16 + 1) : 0);
+        for (int k = 0; k < refs; ++k) t.push_back(draw(pages));
+        o.push_back((int32_t)t.size());
+      };
+      const int n = 1 + draw(3), nd = draw(3);
+      for (int i = 0; i < nd; ++i) holder(pre, pre_tab, pre_off, 2);
+      for (int i = 0; i < n; ++i) holder(len, tab, off, 3), q_len.push_back(len.back() ? 1 : 0);
+      const salt_seq_batch b{n, q_len.data(), len.data(), off.data(), tab.data(), nullptr, nd, pre.data(), pre_off.data(), pre_tab.data()};
+      const uint32_t before = w.kv->stamps;
+      need(salt_seqs_set(w.c, w.q, &b, nullptr) == SALT_OK, "set", round, batch);
+      need((int)w.q->shared == -1 && w.kv->stamps == before + 1, "pages are looked at by salt_seqs_set", round, batch);
+      int seen[64] = {};
+      bool want = false;
+      for (int i = 0; i < nd; ++i)
+        for (int k = 0; k < (pre[i] + 15) / 16; ++k) seen[pre_tab[pre_off[i] + k]] = 1;
+      for (int i = 0; i < n; ++i)
+        for (int k = 0; k < (len[i] + 15) / 16; ++k) want |= seen[tab[off[i] + k]]++ > 0;
+      if (!w.kv->marks) {
+        need(salt_kv_evict(w.c, w.q, 0, 1, 1, nullptr) == SALT_ERR_BAD_STATE, "not tracked", round, batch);
+        if (batch == 2) need(salt_kv_track(w.c, w.kv) == SALT_OK, "salt_kv_track");     // (behind the batch)
+      }
+      if (!w.kv->marks) continue;
+      need(salt_kv_read_marks(w.c, w.q, 0, F, I, nullptr) == SALT_OK && w.kv->stamps == before + 1, "marks that are read", round, batch);
+      // a refused batch, and other work on the cache's stamps, in between
+      const int32_t bad = -1, src = 0, dst = 1;
+      const salt_seq_batch no{1, &bad, &bad, off.data(), tab.data(), nullptr, 0, nullptr, nullptr, nullptr};
+      need(salt_seqs_set(w.c, w.q, &no, nullptr) != SALT_OK, "a refused batch", round, batch);
+      need(salt_kv_copy(w.c, w.kv, 1, &src, &dst, nullptr, nullptr) == SALT_OK, "copy", round, batch);
+      refused += want;
+      uint32_t after = 0;
+      for (int again = 0; again < 3; ++again) {
+        const salt_status ok = want ? SALT_ERR_INVALID_ARG : SALT_OK;
+        need(salt_kv_score(w.c, w.q, 0, g_buf, 0, nullptr, 1.f, 0, nullptr) == ok, "score", round, batch);
+        need(salt_kv_evict(w.c, w.q, 1, 1, 1, nullptr) == ok, "evict", round, batch);
+        need(salt_kv_write_marks(w.c, w.q, 0, F, I, nullptr) == ok, "marks", round, batch);
+        if (again) need(w.kv->stamps == after, "a batch is looked at once", round, batch);
+        after = w.kv->stamps;
+      }
+    }
+    if (round == 200) g_seed = 7;
+  }
+  need(refused > 100 && refused < 700, "batches of either kind", refused);
+  // stamps that start again
+  World w(true);
+  need(w.set({1, 1}, {20, 20}, {0, 1, 2, 3}) == SALT_OK, "set");
+  w.kv->stamps = UINT32_MAX;
+  for (uint32_t& s : w.kv->stamp) s = 1;
+  need(salt_kv_evict(w.c, w.q, 0, 3, 1, nullptr) == SALT_OK && w.kv->stamps == 1, "stamps from the start");
+  w.kv->stamps = UINT32_MAX;
+  for (uint32_t& s : w.kv->stamp) s = 1;
+  need(w.set({1, 1}, {20, 20}, {0, 1, 2, 1}) == SALT_OK && salt_kv_write(w.c, w.q, 0, g_buf, 0, g_buf, 0, nullptr) == SALT_ERR_INVALID_ARG,
+       "writes of two sequences into one page");
+  w.kv->stamps = UINT32_MAX;
+  for (uint32_t& s : w.kv->stamp) s = 1;
+  const int32_t src = 5, dst = 6;
+  need(salt_kv_copy(w.c, w.kv, 1, &src, &dst, nullptr, nullptr) == SALT_OK, "a copy where stamps start again");
+  std::printf("ok\n");
+  return 0;
+}
+
 int main(int argc, char** argv) {
   if (argc == 2 && !strcmp(argv[1], "written")) return written();
+  if (argc == 2 && !strcmp(argv[1], "shared")) return shared();
   return 2;
 }
