@@ -4,6 +4,7 @@
 //             marks of the layer were not given before.
 //   shared    a batch with a page of two sequences, or of a sequence and a domain, is refused by the calls that change
 //             marks; its pages are looked at when such a call comes, once for a batch, and not by salt_seqs_set.
+//   range     evictions of sequences up to 2^19 tokens are launched, of longer ones refused.
 // Prints the first failure and exits 1, else "ok".
 #include <hip/hip_runtime.h>
 
@@ -32,6 +33,7 @@ struct salt_ctx {
 };
 static int g_launches = 0;
 static salt::KvWriteArgs g_write;
+static salt::EvictArgs g_evict;
 namespace salt {
 salt_status ctx_live(salt_ctx* c) { return c ? SALT_OK : SALT_ERR_INVALID_ARG; }
 CtxView ctx_view(const salt_ctx*) { return CtxView{0, 256, 1, 16, 1, kTables}; }
@@ -55,7 +57,7 @@ hipError_t launch_attend(const AttArgs&, int, hipStream_t) { return ++g_launches
 hipError_t launch_rotate(const RotateArgs&, int, int, hipStream_t) { return ++g_launches, hipSuccess; }
 hipError_t launch_score(const ScoreArgs&, int, hipStream_t) { return ++g_launches, hipSuccess; }
 hipError_t launch_marks(const MarksArgs&, bool, hipStream_t) { return ++g_launches, hipSuccess; }
-hipError_t launch_evict(const EvictArgs&, hipStream_t) { return ++g_launches, hipSuccess; }
+hipError_t launch_evict(const EvictArgs& a, hipStream_t) { return g_evict = a, ++g_launches, hipSuccess; }
 hipError_t launch_beam(const BeamArgs&, int, hipStream_t) { return ++g_launches, hipSuccess; }
 hipError_t launch_copy(const CopyArgs&, hipStream_t) { return ++g_launches, hipSuccess; }
 }  // namespace salt
@@ -116,6 +118,22 @@ static int written() {
   need(plain.set({2}, {40}, {0, 1, 2}) == SALT_OK && plain.write(0) == SALT_OK && !g_write.place, "an untracked cache");
   need(salt_kv_track(plain.c, plain.kv) == SALT_OK && plain.write(0) == SALT_OK && g_write.place && g_write.place[1] == 39,
        "tracked behind the batch");
+  std::printf("ok\n");
+  return 0;
+}
+
+static int range() {
+  const int most = 1 << 19;
+  World w(true, most / 16 + 3);
+  std::vector<int32_t> pages;
+  for (int i = 0; i < most / 16 + 3; ++i) pages.push_back(i);
+  need(w.set({0, 1}, {most, 9}, pages) == SALT_OK && salt_kv_evict(w.c, w.q, 0, most - 1, 5, nullptr) == SALT_OK, "2^19 tokens");
+  need(g_evict.max_len == most && g_evict.keep == most - 1, "eviction's arguments", g_evict.max_len, g_evict.keep);
+  const int n = g_launches;
+  need(w.set({0, 1}, {most + 1, 9}, pages) == SALT_OK, "set");
+  for (int keep : {1, 9, most})
+    need(salt_kv_evict(w.c, w.q, 0, keep, 0, nullptr) == SALT_ERR_OUT_OF_RANGE, "2^19 + 1 tokens", keep);
+  need(salt_kv_evict(w.c, w.q, 0, most + 1, 0, nullptr) == SALT_OK && g_launches == n, "nothing to evict");
   std::printf("ok\n");
   return 0;
 }
@@ -196,5 +214,6 @@ static int shared() {
 int main(int argc, char** argv) {
   if (argc == 2 && !strcmp(argv[1], "written")) return written();
   if (argc == 2 && !strcmp(argv[1], "shared")) return shared();
+  if (argc == 2 && !strcmp(argv[1], "range")) return range();
   return 2;
 }

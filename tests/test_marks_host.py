@@ -23,7 +23,7 @@ def marks_host(tmp_path_factory):
 
 
 @pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
-@pytest.mark.parametrize("check", ["written", "shared"])
+@pytest.mark.parametrize("check", ["written", "shared", "range"])
 def test_marks_host(marks_host, check):
     res = subprocess.run([marks_host, check], capture_output=True, text=True, timeout=120)
     assert res.returncode == 0 and res.stdout.strip().endswith("ok"), res.stdout + res.stderr
