@@ -598,7 +598,10 @@ SALT_API void salt_beams_destroy(salt_ctx* ctx, salt_beams* beams);
  * and token, each [n_reqs][n_out] (device).  A beam with a score that is not finite (-inf: one that is not live), with a
  * logit of NaN or +inf, or with none above -inf offers nothing, and no beam offers a token of logit -inf; where
  * there are too few, the rest are (-inf, -1, -1).  The order within a beam is exactly that of the logits; exponentials are
- * fp32, their sum and the worth 64 bits (the worth rounded to fp32 on output).
+ * fp32, their sum and the worth 64 bits (the worth rounded to fp32 on output).  A beam's log-sum, and with it its
+ * worths, is off by at most 2^-24 (1.6 log2 vocab + 17 + vocab / 2048), 6.4e-6 at 2^17 tokens, and by some 1e-7 where logits do
+ * not rise all through the row: continuations of two beams that are worth the same to that may come in either
+ * order (beams with the same logits and score are worth the same to the bit).
  * Errors: SALT_ERR_OUT_OF_RANGE (counts), SALT_ERR_INVALID_ARG (pointers, rows), SALT_ERR_BAD_STATE (capture, as
  * salt_base_product). */
 SALT_API salt_status salt_beam_select(salt_ctx* ctx, salt_beams* beams, int32_t n_reqs, int32_t width, int32_t vocab,
