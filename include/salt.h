@@ -419,7 +419,7 @@ typedef struct {
 typedef struct salt_kv salt_kv;
 typedef struct salt_seqs salt_seqs;
 
-/* Bytes of the pool (host-only; 0 for an invalid configuration). */
+/* Bytes of the pool (host-only; 0 for an invalid configuration), without the marks of a tracked cache. */
 SALT_API size_t salt_kv_bytes(const salt_kv_config* cfg);
 /* The pool is allocated and cleared by the call and owned by the context (freed by salt_kv_destroy
  * or salt_destroy; salt_kv_destroy waits for the device).  k, v, q and out are in the context's
@@ -543,8 +543,9 @@ SALT_API salt_status salt_rotate(salt_ctx* ctx, const salt_rotation* rot, int32_
  * prompt but the last, say).  Where salt_kv_write_marks gave the batch's marks of the layer first, they stay.
  * (Behind an eviction a place is no position any more: there a step is scored with pos, or given its marks.)
  *
- * salt_kv_track allocates the marks of every layer and page and clears them (blocking, once, before work of the
- * cache is recorded into a graph; a second call does nothing).  Errors: SALT_ERR_INVALID_ARG, SALT_ERR_OUT_OF_MEMORY. */
+ * salt_kv_track allocates the marks of every layer and page, 8 bytes a token and kv head (each layer's two arrays rounded up
+ * to 256 bytes), and clears them (blocking, once, before work of the cache is recorded into a graph; a second call
+ * does nothing).  Errors: SALT_ERR_INVALID_ARG, SALT_ERR_OUT_OF_MEMORY. */
 SALT_API salt_status salt_kv_track(salt_ctx* ctx, salt_kv* kv);
 /* After salt_kv_write of the step, with the q and scale of salt_attend: to token j of a sequence, for each
  * kv head, add
@@ -583,7 +584,9 @@ SALT_API salt_status salt_kv_write_marks(salt_ctx* ctx, salt_seqs* seqs, int32_t
  * of all of them:
  *     salt_beam_select, [the host reads the beams], salt_kv_copy of the last pages of beams that go on
  *     more than once, salt_seqs_set with the new page tables.
- * (A full page may stand in the tables of several sequences; the one that new tokens go into may not.)
+ * (A full page may stand in the tables of several sequences; the one that new tokens go into may not.  Beams that share
+ * pages are not scored or evicted: salt_kv_score, salt_kv_evict and salt_kv_write_marks refuse their batch.  A request
+ * that is to have both copies the full pages, too, so that each of its sequences has its own.)
  *
  * salt_beams is an object that owns scratch for up to max_rows beams (at most 65536) of a call and max_out (at most
  * 64) continuations of a request; its work is ordered by the library across streams, as that of salt_seqs. */
@@ -591,7 +594,8 @@ typedef struct salt_beams salt_beams;
 SALT_API salt_status salt_beams_create(salt_ctx* ctx, int32_t max_rows, int32_t max_out, salt_beams** out);
 SALT_API void salt_beams_destroy(salt_ctx* ctx, salt_beams* beams);
 /* n_reqs requests of `width` beams each (1 to 64), logits [n_reqs * width][ld] (device, context dtype, 16-byte
- * aligned; ld 0: dense, else a multiple of 8; vocab in [1, 2^24]), score [n_reqs * width] (device, fp32) the beams' own log
+ * aligned; ld a multiple of 8, also where 0 makes the rows dense: a vocabulary that is none has padded rows; vocab in
+ * [1, 2^24]), score [n_reqs * width] (device, fp32) the beams' own log
  * probabilities.  Of a request's continuations (beam b, token v), worth
  *     score[b] + logits[b][v] - log sum_u exp logits[b][u],
  * the n_out best in order, ties by the lower beam, then the lower token: their worth, beam (0 to width - 1)
@@ -599,7 +603,7 @@ SALT_API void salt_beams_destroy(salt_ctx* ctx, salt_beams* beams);
  * logit of NaN or +inf, or with none above -inf offers nothing, and no beam offers a token of logit -inf; where
  * there are too few, the rest are (-inf, -1, -1).  The order within a beam is exactly that of the logits; exponentials are
  * fp32, their sum and the worth 64 bits (the worth rounded to fp32 on output).  A beam's log-sum, and with it its
- * worths, is off by at most 2^-24 (1.6 log2 vocab + 17 + vocab / 2048), 6.4e-6 at 2^17 tokens, and by some 1e-7 where logits do
+ * worths, is off by at most 2^-24 (1.6 log2 vocab + 17 + vocab / 2048), 6.5e-6 at 2^17 tokens, and by some 1e-7 where logits do
  * not rise all through the row: continuations of two beams that are worth the same to that may come in either
  * order (beams with the same logits and score are worth the same to the bit).
  * Errors: SALT_ERR_OUT_OF_RANGE (counts), SALT_ERR_INVALID_ARG (pointers, rows), SALT_ERR_BAD_STATE (capture, as
