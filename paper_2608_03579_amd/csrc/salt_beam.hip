@@ -79,8 +79,9 @@ __device__ __forceinline__ float largest(const float (&v)[16]) {
 
 // One piece of one row: a block of four waves, which take runs of 1024 logits in turn, 16 to a lane.  A lane's
 // maximum decides whether its logits are looked at, and the waves tell each other bounds, so that few of them enter a
-// list only to leave it.  512 rows of 128256 logits in bf16, 16 continuations: 45 us (2.9 TB/s), bound by the vector unit
-// (27 us of it: 225 instructions to a run, 16 of them exponentials) beside the bytes (25 us).  Lists entered value by
+// list only to leave it.  512 rows of 128256 logits in bf16, 16 continuations: 45 us under the profiler (2.9
+// TB/s), in fp32 48 (5.5 TB/s).  Of the 45 the vector unit is busy for 27 (225 instructions to a run, 16 of them exponentials)
+// and the bytes take 25 at a copy's rate: neither bounds it, they overlap badly.  Lists entered value by
 // value took 157 us, by ballot 56, with bounds between waves 45; twice or half as many blocks to a row 52.  Four rows:
 // 8 us, a chain of launch, load and list.
 constexpr int kRun = 1024;

@@ -8,7 +8,8 @@
 // Sixteen lanes hold one vector pair (k, v): one pass over the data, the maximum by
 // four lane exchanges.  Bound by memory traffic and, for a decode step, by the launch: 256 tokens of
 // 8 x 128 values written in 3.3 us, 8192 in 12.4 (4.2 TB/s of k, v and codes), 70 MB of codes read back as
-// 133 MB of bf16 in 32 to 44 us (4.7 to 6.3 TB/s from card to card).
+// 133 MB of bf16 in 32 to 44 us (4.7 to 6.3 TB/s from card to card).  A tracked cache's marks start with the write: 3.4 us
+// for 3.2, 9.7 for 9.1.
 #include <hip/hip_runtime.h>
 
 #include "salt_device.h"

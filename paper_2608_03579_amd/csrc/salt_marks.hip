@@ -12,9 +12,11 @@
 // mark has one owner and is written once, so no atomics, and the sum's order is fixed.
 // Codes are exact in bf16; q enters as it is in bf16 contexts, in three bf16 terms (24 bits) in fp32 ones.
 // The attention itself has the maxima and sums, but keeps them in its work items; taking them from there would tie a
-// layer's score to its attention.  Measured with 32 heads in 8 groups: 64 sequences of up to 4096 keys, one token each,
-// 11.8 + 10.8 us (31 MB of keys read twice, the second time from the Infinity Cache); two prompts of 4096 tokens, 215 +
-// 230 us for 2 x 137 GFLOP.
+// layer's score to its attention.  Measured with 32 heads in 8 groups, a kernel by itself under the profiler, on inputs
+// repeated: 64 sequences of up to 4096 keys, one token each, 11.8 + 10.8 us (31 MB of keys read twice, the second time
+// from the Infinity Cache); two prompts of 4096 tokens, 215 + 230 us for 2 x 137 GFLOP, 64 + 16 where their last 64 tokens
+// count; in fp32 423 + 567, of heads of 256 1041 + 1110.  The calls on fresh inputs, marks in and out among them: 28 and
+// 392 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -64,7 +66,6 @@ __device__ __forceinline__ void wave_order() {
 template <int kBytes>
 struct Staged {
   static constexpr int kChunks = kBytes / 16;              // of a row
-  static constexpr int kRowsAtOnce = 64 / (kChunks < 64 ? kChunks : 64);
   static __device__ __forceinline__ int at(int row, int chunk) {
     constexpr int kWindow = kChunks < 16 ? 16 / kChunks : 1;   // rows that 256 bytes hold
     return row * kBytes + 16 * (chunk ^ ((row / kWindow) & (kChunks - 1) & 15));
@@ -149,10 +150,10 @@ __device__ __forceinline__ float2 row_final(float m, float l) {
 // One item: RT row tiles of 16 to a wave, WR waves side by side over the rows and WK over the keys, 32 keys in turn.
 // (WK = WR = 1: one wave alone.)  Each lane has a running maximum and sum of its own keys, joined over lanes and
 // waves in the end.  A logit is an fma against the maximum so far, which follows the largest one only when that
-// is kMaxSlack above it.  Few rows are bound by latency.  Many are bound by the vector unit: 27 instructions to 16 keys x
-// 16 rows, four of them exponentials at a quarter of the rate, and the matrix unit beside them for 40 % of the time.  Four row
-// tiles to a wave where registers allow: codes are converted once for all (two tiles: 237 to 269 us for 215), and one
-// test for all of them whether a maximum has to follow (a test for each: 240 us).
+// is kMaxSlack above it.  Few rows are bound by latency.  Many keep the vector unit busy for 58 % of the time (27
+// instructions to 16 keys x 16 rows, four of them exponentials at a quarter of the rate) and the matrix unit for 29 %; the
+// rest are waits of two waves to a SIMD.  Four row tiles to a wave where registers allow: codes are converted once for
+// all (two tiles: 237 to 269 us for 215), and one test for all of them whether a maximum has to follow (a test for each: 240 us).
 template <typename E, int D, int FMT, int RT, int WR, int WK>
 __device__ __forceinline__ void stat_item(const ScoreArgs& sa, const AttItem& it, int kvh, uint8_t* stage, float* lds) {
   const AttArgs& a = sa.att;
@@ -527,8 +528,9 @@ __global__ void __launch_bounds__(256, sizeof(E) * D <= 256 ? 2 : 1) k_score_few
 }
 
 // Sequences of many counted rows: a block to a unit and kv head, whose waves take 16 rows in turn, the next ones on
-// their way; their sums meet in LDS.  Bound by the vector unit (75 instructions to 64 keys x 16 rows) and by waits for
-// rows and LDS that two waves to a SIMD do not hide.  A wave to a unit, rows not shared out: 911 us for 230.
+// their way; their sums meet in LDS.  Bound by waits for rows and LDS that two waves to a SIMD do not hide: the vector unit
+// (75 instructions to 64 keys x 16 rows) is busy for 39 % of the time, the matrix unit for 28 %.  A wave to a unit, rows
+// not shared out: 911 us for 230.
 template <typename E, int D, int FMT>
 __global__ void __launch_bounds__(256, sizeof(E) * D <= 256 ? 2 : 1) k_score_many(ScoreArgs sa) {
   const AttArgs& a = sa.att;
@@ -690,6 +692,9 @@ __global__ void __launch_bounds__(256) k_marks(MarksArgs a) {
 // largest, and the kept ones behind place `keep` go to the places of the dropped ones before it, in order.
 // No two moves touch one place.  A block's chain of steps bounds it, not the bytes: up to kEvictShort tokens have
 // their marks read once, into registers (k_evict); longer sequences go through memory again in each step (k_evict_long).
+// Under the profiler: 16 sequences of 8192 tokens and 8 kv heads x 128 down to 512, 24.4 us on 128 of the 256 compute units
+// (the blocks of 1024 threads keep 98 scalar registers, of ballots, in vector lanes, which lengthens the chain);
+// 40 of 257 down to 256, 8.3 us.
 constexpr uint32_t kProtected = 0xffffffffu, kNanKey = 0xfffffffeu;
 __device__ __forceinline__ uint32_t weight_order(float w) {
   if (w != w) return kNanKey;
@@ -885,7 +890,9 @@ __global__ void __launch_bounds__(NT) k_evict(EvictArgs a) {
   }
 }
 
-// The same for longer sequences: a bit for each token in LDS says which stay, and moves are listed kMoves at a time.
+// The same for longer sequences: a bit for each token in LDS says which stay, and moves are listed kMoves at a time, each
+// list by going through all bits again.  Two sequences of 131072 tokens and 8 kv heads x 128 down to 4096: 489 us; one
+// head of 2^19 down to 2^18, 131072 moves, 11.5 ms.
 constexpr int kMoves = 2048;
 struct alignas(16) EvictLongLds {                          // dynamic LDS: these, and the bits
   uint32_t hist[kBins];

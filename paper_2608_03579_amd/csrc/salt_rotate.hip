@@ -7,8 +7,9 @@
 //
 // one rounding at the end.  The angle is taken in revolutions and reduced in 64 bits: at a position of 10^6 an
 // fp32 product is off by 0.06 radians.  Reduced to half a revolution it is rounded once (2^-24 of it).
-// Bound by memory traffic: 8192 tokens of 32 + 8 heads of 128 in bf16 (168 MB) in 30.5 us, 5.5 TB/s; one token in
-// 3.8 us, a launch and two rounds to memory.  (A head's values asked for ahead of the angles: 4.4 us.)
+// Bound by memory traffic: 8192 tokens of 32 + 8 heads of 128 in bf16 (168 MB) in 39.4 us on fresh inputs, 4.3 TB/s (a
+// large copy: 5.2), and 30.5 where the 84 MB of the inputs come from the Infinity Cache; one token in 3.8 us, a launch
+// and two rounds to memory.  (A head's values asked for ahead of the angles: 4.4 us.)
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
