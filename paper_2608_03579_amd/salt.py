@@ -604,7 +604,7 @@ class Seqs:
         return lib.salt_kv_write(self.ctx.h, self.h, layer, k_ptr, ldk, v_ptr, ldv, stream)
 
     def write(self, layer: int, k_ptr: int, v_ptr: int, stream: int = 0, ldk: int = 0, ldv: int = 0):
-        """The step's k and v of `layer` into the cache."""
+        """The step's k and v of `layer` into the cache (marks of a tracked one start: weight 0, place in the sequence)."""
         self.ctx._check(self.write_status(layer, k_ptr, v_ptr, stream, ldk, ldv), "salt_kv_write")
 
     def read_status(self, layer: int, what: str, k_ptr: int, v_ptr: int, stream: int = 0, ldk: int = 0,
